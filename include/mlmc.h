@@ -55,15 +55,19 @@ typedef enum {
 #define MLMC_DEV_CAPACITY 1  /* row_off[M] > capacity: entries past capacity were not written */
 #define MLMC_DEV_NONFINITE 2 /* an Inf or NaN input was seen (it is ordered by its bit pattern) */
 #define MLMC_DEV_INTERNAL 4  /* an internal consistency check failed (counts do not add up) */
+#define MLMC_DEV_RANGE 16    /* mlmc_distill: a teacher's index is not below the vocabulary */
 #define MLMC_DEV_REDONE 8    /* not an error: a row's sampled threshold search was refuted and the row was redone exactly */
 
 typedef enum { MLMC_F32 = 0, MLMC_BF16 = 1 } mlmc_dtype;
 typedef enum { MLMC_TOPK = 0, MLMC_BITS = 1, MLMC_FBITS = 2, MLMC_STOPK = 3, MLMC_VBITS = 4, MLMC_RTN = 5 } mlmc_kind;
 
+typedef enum { MLMC_ACT_NONE = 0, MLMC_ACT_RELU = 1, MLMC_ACT_GELU = 2 } mlmc_act; /* gelu(z) = z (1 + erf(z / sqrt 2)) / 2 */
+
 #define MLMC_MAX_LEVELS 32   /* L <= 32 */
 #define MLMC_MAX_WORKERS 1024 /* M <= 1024 */
 #define MLMC_MAX_SLEVELS 65536 /* MLMC_STOPK: L = ceil(d / s) <= 65536 */
 #define MLMC_MAX_RTN_LEVELS 8  /* MLMC_RTN: L <= 8 */
+#define MLMC_MAX_TEACHER 1024  /* mlmc_distill: entries of a row's teacher */
 #define MLMC_TILE 4096       /* elements per tile of the per-row offset table */
 
 /*
@@ -284,6 +288,86 @@ mlmc_status mlmc_aggregate_update(const mlmc_plan_t *plan, const int32_t *level,
  *   level: dev [M] int32 as written by a compress call;  bits: dev [M] uint64 (out).
  */
 mlmc_status mlmc_message_bits(const mlmc_plan_t *plan, const int32_t *level, uint64_t *bits, void *hip_stream);
+
+/*
+ * What a worker computes before it has a gradient: layer norm, the linear layer, the distillation loss, each with its
+ * gradient.  They need no plan.  Weight gradients are written in fp32 or bf16 (grad_dtype) at any place that is aligned to an entry, so
+ * that a worker's tensors can lie one behind the other in its row of the matrix g that the compress calls read.
+ * Conventions beside those at the top:
+ *   - A matrix is row-major with the row distance given behind its pointer (in entries, at least its width); rows need no alignment beyond
+ *     that of an entry.  dtype: MLMC_F32 or MLMC_BF16, of all matrices of a call but the weight gradients; weight and bias of the
+ *     layer norm and the bias of the linear layer are fp32.
+ *   - Sums, statistics and the intermediate values are fp32; every output is rounded once, to nearest, ties to even.  Results are a pure
+ *     function of the inputs: sums have an order that depends on sizes, types and alignment alone.
+ *   - rows may be 0: nothing but weight gradients (zeros) is written, and the matrices of rows may be NULL.
+ *   - ws: dev scratch, 256-byte aligned, of ws_bytes >= what the _workspace function next to the call returns for the sizes (host; 0 also for
+ *     sizes that the call refuses); NULL where that is 0.
+ *   - Outputs do not overlap inputs, except where a call says that they may be the same matrix (same pointer and row distance).
+ */
+
+/*
+ * Layer norm of every row: y_j = (x_j - mu) r weight_j + bias_j, mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps).
+ *   x: dev [rows][ldx];  weight, bias: dev [d] or NULL (1, 0);  eps >= 0;  y: dev [rows][ldy] (out; may be x);
+ *   stats: dev [rows][2] fp32 (out) or NULL: mu and r, for the backward pass.
+ */
+mlmc_status mlmc_layer_norm(const void *x, int64_t ldx, int64_t rows, int64_t d, int dtype, const float *weight, const float *bias,
+                            float eps, void *y, int64_t ldy, float *stats, void *hip_stream);
+
+/*
+ * Its gradient.  With h_j = (x_j - mu) r and c_j = dy_j weight_j: dx_j = r (c_j - mean c - h_j mean(c h)); dweight_j = sum over
+ * rows of dy_j h_j; dbias_j = sum over rows of dy_j.
+ *   dy, x: dev [rows][..];  stats: as mlmc_layer_norm wrote it;  dx: dev [rows][lddx] (out; may be dy or x);
+ *   dweight, dbias: dev [d] of grad_dtype (out), either or both NULL (ws is not needed with both).
+ */
+size_t mlmc_layer_norm_workspace(int64_t rows, int64_t d);
+mlmc_status mlmc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t rows, int64_t d, int dtype,
+                                     const float *weight, const float *stats, void *dx, int64_t lddx, void *dweight, void *dbias,
+                                     int grad_dtype, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Linear layer with its epilogue: v = x weight^T + bias, y = act(v) + residual.
+ *   x: dev [rows][inputs];  weight: dev [outputs][inputs];  bias: dev [outputs] or NULL;  residual: dev [rows][outputs] or NULL;
+ *   z: dev [rows][outputs] (out) or NULL: receives v, which the gradient of the activation needs;  y: dev [rows][outputs] (out; may be
+ *   residual).  0 <= rows, 1 <= outputs, inputs, each at most 2^21.  The workspace is that of all three calls.
+ */
+size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs);
+mlmc_status mlmc_linear(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
+                        const float *bias, int act, const void *residual, int64_t ldr, void *z, int64_t ldz, void *y, int64_t ldy,
+                        void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gradient with respect to the layer's input, through the activation before it: dx = (dy weight) act'(z) + residual.
+ *   dy: dev [rows][outputs];  z: dev [rows][inputs], the v of the layer whose activation made x (not read for MLMC_ACT_NONE: then dx is
+ *   the gradient of x itself);  residual: dev [rows][inputs] or NULL: a gradient that comes by another way;  dx: dev [rows][inputs]
+ *   (out; may be residual or z).  act'(z) of relu is 0 at z = 0.
+ */
+mlmc_status mlmc_linear_dgrad(const void *dy, int64_t lddy, const void *weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs,
+                              int dtype, int act, const void *z, int64_t ldz, const void *residual, int64_t ldr, void *dx, int64_t lddx,
+                              void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gradient with respect to weight and bias: dweight = dy^T x, dbias = sum over rows of dy, dy being the gradient of v.
+ *   dweight: dev [outputs][lddw] of grad_dtype (out);  dbias: dev [outputs] of grad_dtype (out) or NULL.
+ */
+mlmc_status mlmc_linear_wgrad(const void *dy, int64_t lddy, const void *x, int64_t ldx, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
+                              void *dweight, int64_t lddw, void *dbias, int grad_dtype, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Distillation from a teacher's top logits.  Row n has a teacher of `top` entries (index i_k, logit t_k); with T = temperature
+ *     q_k = exp(t_k / T) / sum exp(t_k' / T) over the entries,  p_j = exp(s_j / T) / sum exp(s_j' / T) over the vocabulary,
+ *     loss_n = T^2 sum_k q_k (log q_k - log p_{i_k}),   dlogits_nj = scale dloss_n T (p_j - sum of the q_k with i_k = j).
+ * With one entry and T = 1 this is the cross entropy with label i_1.
+ *   logits: dev [rows][vocab];  t_idx, t_val: dev [rows][top], 1 <= top <= MLMC_MAX_TEACHER; entries of an index below 0 are padding (their
+ *   t_val is not used).  A row without an entry, or with none above -Inf, is masked: its logits are not read, loss and gradient are 0.
+ *   An index >= vocab makes the row's loss NaN, its gradient 0, and sets MLMC_DEV_RANGE.  A logit of -Inf has p = 0; NaN, +Inf or nothing
+ *   but -Inf among a row's logits make its loss and gradient NaN.
+ *   dloss: dev [rows] fp32 or NULL (1); a row whose scale * dloss is 0 has gradient 0, whatever its logits.
+ *   loss: dev [rows] fp32 (out);  dlogits: dev [rows][ldd] (out; may be logits) or NULL: the loss alone;  dev_status: dev [1] or NULL.
+ */
+size_t mlmc_distill_workspace(int64_t rows, int64_t vocab, int top);
+mlmc_status mlmc_distill(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const int32_t *t_idx, const float *t_val, int top,
+                         float temperature, const float *dloss, float scale, float *loss, void *dlogits, int64_t ldd, int32_t *dev_status,
+                         void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
  * Per-kernel timing for benchmarks (measurement aid, not part of the method).  While enabled, every kernel

@@ -17,15 +17,19 @@ LIB_PATH = os.path.join(_PKG, "libmlmc.so")
 
 MLMC_OK, MLMC_EINVAL, MLMC_ENOMEM, MLMC_EHIP, MLMC_ELIMIT = 0, 1, 2, 3, 4
 MLMC_STATIC_SCRATCH_BYTES = 1 << 20
-MLMC_DEV_CAPACITY, MLMC_DEV_NONFINITE, MLMC_DEV_INTERNAL, MLMC_DEV_REDONE = 1, 2, 4, 8
+MLMC_DEV_CAPACITY, MLMC_DEV_NONFINITE, MLMC_DEV_INTERNAL, MLMC_DEV_REDONE, MLMC_DEV_RANGE = 1, 2, 4, 8, 16
 MLMC_F32, MLMC_BF16 = 0, 1
 MLMC_TOPK, MLMC_BITS, MLMC_FBITS, MLMC_STOPK, MLMC_VBITS, MLMC_RTN = 0, 1, 2, 3, 4, 5
+MLMC_ACT_NONE, MLMC_ACT_RELU, MLMC_ACT_GELU = 0, 1, 2
 MLMC_MAX_SLEVELS = 65536
+MLMC_MAX_TEACHER = 1024
 MLMC_TILE = 4096
 MLMC_MAX_LEVELS = 32
 
 EXPORTS = ["mlmc_plan", "mlmc_plan_destroy", "mlmc_plan_set_sampling", "mlmc_plan_set_staging", "mlmc_plan_set_overlap", "mlmc_plan_num_tiles", "mlmc_plan_chunk", "mlmc_plan_num_planes", "mlmc_geometric_p",
            "mlmc_status_string", "mlmc_level_norms", "mlmc_compress_topk", "mlmc_compress_bits", "mlmc_compress_bits_static", "mlmc_compress_rtn", "mlmc_aggregate", "mlmc_aggregate_update", "mlmc_message_bits",
+           "mlmc_layer_norm", "mlmc_layer_norm_workspace", "mlmc_layer_norm_backward", "mlmc_linear", "mlmc_linear_workspace", "mlmc_linear_dgrad", "mlmc_linear_wgrad",
+           "mlmc_distill", "mlmc_distill_workspace",
            "mlmc_profile_enable", "mlmc_profile_reset", "mlmc_profile_num_kernels", "mlmc_profile_kernel_name",
            "mlmc_profile_get"]
 
@@ -81,6 +85,18 @@ def lib():
         L.mlmc_aggregate_update.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, vp, C.c_float, C.c_float, vp, vp, vp, vp]
         L.mlmc_message_bits.restype = C.c_int
         L.mlmc_message_bits.argtypes = [vp, vp, vp, vp]
+        f32, sz = C.c_float, C.c_size_t
+        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64]), ("mlmc_distill_workspace", [i64, i64, i32])):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = args
+        for name, args in (("mlmc_layer_norm", [vp, i64, i64, i64, i32, vp, vp, f32, vp, i64, vp, vp]),
+                           ("mlmc_layer_norm_backward", [vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, i64, vp, vp, i32, vp, sz, vp]),
+                           ("mlmc_linear", [vp, i64, vp, i64, i64, i64, i64, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, sz, vp]),
+                           ("mlmc_linear_dgrad", [vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, sz, vp]),
+                           ("mlmc_linear_wgrad", [vp, i64, vp, i64, i64, i64, i64, i32, vp, i64, vp, i32, vp, sz, vp]),
+                           ("mlmc_distill", [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, f32, vp, vp, i64, vp, vp, sz, vp])):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = args
         L.mlmc_profile_enable.restype = None
         L.mlmc_profile_enable.argtypes = [i32]
         L.mlmc_profile_reset.restype = None
@@ -327,3 +343,177 @@ def mlmc_message_bits(plan: Plan, msg, bits: Optional[torch.Tensor] = None) -> t
     _check(lib().mlmc_message_bits(plan.handle, _ptr(msg.level), _ptr(bits), _stream()), "mlmc_message_bits")
     return bits
 
+
+
+# ---- a worker's own step: layer norm, linear layer, distillation loss ------------------------------------------------
+_DTYPE = {torch.float32: MLMC_F32, torch.bfloat16: MLMC_BF16}
+
+
+def _rows(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
+    """Row distance of a matrix on the current device with unit inner stride; raises for anything else."""
+    sh = t.shape
+    if len(sh) != 2 or not t.is_cuda or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype) or (shape is not None and (sh[0] != shape[0] or sh[1] != shape[1])):
+        want = "float32 or bfloat16" if dtype is None else str(dtype)
+        raise MlmcError(f"{name} must be a CUDA matrix of {want}" + ("" if shape is None else f", [{shape[0]}, {shape[1]}]"))
+    if t.get_device() != torch.cuda.current_device():
+        raise MlmcError(f"{name} is not on the current device")
+    n, d = sh
+    r, c = t.stride()
+    if (c != 1 and d > 1) or (r < d and n > 1):
+        raise MlmcError(f"{name} must have unit inner stride and rows that do not overlap")
+    return r if n > 1 and r > d else d
+
+
+def _vector(t: Optional[torch.Tensor], name: str, d: int, dtype=torch.float32):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != d or not t.is_contiguous() or not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise MlmcError(f"{name} must be a contiguous CUDA tensor of {dtype}, [{d}], on the current device")
+    return t.data_ptr()
+
+
+def _scratch(ws: Optional[torch.Tensor], need: int, device):
+    """The caller's workspace, or one of this call (from torch's allocator, on the current stream)."""
+    if need == 0:
+        return None, 0
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    elif ws.dtype != torch.uint8 or not ws.is_cuda or not ws.is_contiguous() or ws.get_device() != torch.cuda.current_device():
+        raise MlmcError("ws must be a contiguous CUDA tensor of torch.uint8 on the current device")
+    return ws, ws.numel()
+
+
+def mlmc_layer_norm_workspace(rows: int, d: int) -> int:
+    return lib().mlmc_layer_norm_workspace(rows, d)
+
+
+def mlmc_linear_workspace(rows: int, outputs: int, inputs: int) -> int:
+    return lib().mlmc_linear_workspace(rows, outputs, inputs)
+
+
+def mlmc_distill_workspace(rows: int, vocab: int, top: int) -> int:
+    return lib().mlmc_distill_workspace(rows, vocab, top)
+
+
+def mlmc_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                    y: Optional[torch.Tensor] = None, with_stats: bool = False, stats: Optional[torch.Tensor] = None):
+    """y, or (y, stats) if the statistics for the backward pass are asked for (with_stats, or a tensor [rows, 2] that receives them)."""
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    if y is None:
+        y = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    if stats is None and with_stats:
+        stats = torch.empty((n, 2), dtype=torch.float32, device=x.device)
+    elif stats is not None and (tuple(stats.shape) != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or not stats.is_cuda):
+        raise MlmcError(f"stats must be a contiguous float32 CUDA tensor [{n}, 2]")
+    rc = lib().mlmc_layer_norm(x.data_ptr(), ldx, n, d, _DTYPE[x.dtype], _vector(weight, "weight", d), _vector(bias, "bias", d), eps,
+                               y.data_ptr(), _rows(y, "y", x.dtype, (n, d)), _ptr(stats), _stream())
+    _check(rc, "mlmc_layer_norm")
+    return y if stats is None else (y, stats)
+
+
+def mlmc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], stats: torch.Tensor,
+                             dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                             dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dx; dweight and dbias ([d], fp32 or bf16 alike, for instance parts of a row of the gradient matrix) are written in place."""
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    if tuple(stats.shape) != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or not stats.is_cuda:
+        raise MlmcError(f"stats must be a contiguous float32 CUDA tensor [{n}, 2]")
+    if dx is None:
+        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    g = torch.float32
+    need = 0
+    if dweight is not None or dbias is not None:
+        g = (dbias if dweight is None else dweight).dtype
+        if g not in _DTYPE:
+            raise MlmcError("dweight and dbias must be of float32 or bfloat16")
+        need = lib().mlmc_layer_norm_workspace(n, d)
+    ws, nbytes = _scratch(ws, need, x.device)
+    rc = lib().mlmc_layer_norm_backward(dy.data_ptr(), _rows(dy, "dy", x.dtype, (n, d)), x.data_ptr(), ldx, n, d, _DTYPE[x.dtype],
+                                        _vector(weight, "weight", d), stats.data_ptr(), dx.data_ptr(), _rows(dx, "dx", x.dtype, (n, d)),
+                                        _vector(dweight, "dweight", d, g), _vector(dbias, "dbias", d, g), _DTYPE[g], _ptr(ws), nbytes, _stream())
+    _check(rc, "mlmc_layer_norm_backward")
+    return dx
+
+
+def mlmc_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = MLMC_ACT_NONE,
+                residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = act(x weight^T + bias) + residual; z, if given, receives what act is applied to."""
+    ldx, ldw = _rows(x, "x"), _rows(weight, "weight", x.dtype)
+    n, k = x.shape
+    m = weight.shape[0]
+    if weight.shape[1] != k:
+        raise MlmcError(f"weight must be [outputs, {k}]")
+    if y is None:
+        y = torch.empty((n, m), dtype=x.dtype, device=x.device)
+    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), x.device)
+    rc = lib().mlmc_linear(x.data_ptr(), ldx, weight.data_ptr(), ldw, n, m, k, _DTYPE[x.dtype], _vector(bias, "bias", m), act,
+                           _ptr(residual), 0 if residual is None else _rows(residual, "residual", x.dtype, (n, m)),
+                           _ptr(z), 0 if z is None else _rows(z, "z", x.dtype, (n, m)),
+                           y.data_ptr(), _rows(y, "y", x.dtype, (n, m)), _ptr(ws), nbytes, _stream())
+    _check(rc, "mlmc_linear")
+    return y
+
+
+def mlmc_linear_dgrad(dy: torch.Tensor, weight: torch.Tensor, act: int = MLMC_ACT_NONE, z: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dx = (dy weight) act'(z) + residual, z being what the activation in front of the layer was applied to."""
+    lddy, ldw = _rows(dy, "dy"), _rows(weight, "weight", dy.dtype)
+    n, m = dy.shape
+    k = weight.shape[1]
+    if weight.shape[0] != m:
+        raise MlmcError(f"weight must be [{m}, inputs]")
+    if act != MLMC_ACT_NONE and z is None:
+        raise MlmcError("the gradient of an activation needs z")
+    if dx is None:
+        dx = torch.empty((n, k), dtype=dy.dtype, device=dy.device)
+    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), dy.device)
+    rc = lib().mlmc_linear_dgrad(dy.data_ptr(), lddy, weight.data_ptr(), ldw, n, m, k, _DTYPE[dy.dtype], act,
+                                 _ptr(z), 0 if z is None else _rows(z, "z", dy.dtype, (n, k)),
+                                 _ptr(residual), 0 if residual is None else _rows(residual, "residual", dy.dtype, (n, k)),
+                                 dx.data_ptr(), _rows(dx, "dx", dy.dtype, (n, k)), _ptr(ws), nbytes, _stream())
+    _check(rc, "mlmc_linear_dgrad")
+    return dx
+
+
+def mlmc_linear_wgrad(dy: torch.Tensor, x: torch.Tensor, dweight: torch.Tensor, dbias: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dweight = dy^T x and, if given, dbias = sum over rows of dy, written in place (fp32 or bf16 alike)."""
+    lddy, ldx = _rows(dy, "dy"), _rows(x, "x", dy.dtype)
+    n, m = dy.shape
+    k = x.shape[1]
+    if x.shape[0] != n:
+        raise MlmcError(f"x must be [{n}, inputs]")
+    lddw = _rows(dweight, "dweight", None, (m, k))
+    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), dy.device)
+    rc = lib().mlmc_linear_wgrad(dy.data_ptr(), lddy, x.data_ptr(), ldx, n, m, k, _DTYPE[dy.dtype], dweight.data_ptr(), lddw,
+                                 _vector(dbias, "dbias", m, dweight.dtype), _DTYPE[dweight.dtype], _ptr(ws), nbytes, _stream())
+    _check(rc, "mlmc_linear_wgrad")
+    return dweight
+
+
+def mlmc_distill(logits: torch.Tensor, t_idx: torch.Tensor, t_val: torch.Tensor, temperature: float = 1.0,
+                 dloss: Optional[torch.Tensor] = None, scale: float = 1.0, grad: bool = True, loss: Optional[torch.Tensor] = None,
+                 dlogits: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """(loss of every row, scale * dloss times its gradient in the logits); the second is None if neither `grad` nor `dlogits` asks for it.
+    dlogits may be the logits themselves.  dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for an index outside the vocabulary."""
+    ldl = _rows(logits, "logits")
+    n, v = logits.shape
+    if (t_idx.dtype != torch.int32 or t_val.dtype != torch.float32 or t_idx.dim() != 2 or t_idx.shape[0] != n or t_val.shape != t_idx.shape
+            or not t_idx.is_contiguous() or not t_val.is_contiguous() or not t_idx.is_cuda or not t_val.is_cuda):
+        raise MlmcError(f"t_idx and t_val must be contiguous CUDA tensors of int32 and float32, [{n}, top]")
+    top = t_idx.shape[1]
+    if dlogits is None and grad:
+        dlogits = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+    if loss is None:
+        loss = torch.empty(n, dtype=torch.float32, device=logits.device)
+    ws, nbytes = _scratch(ws, lib().mlmc_distill_workspace(n, v, top), logits.device)
+    rc = lib().mlmc_distill(logits.data_ptr(), ldl, n, v, _DTYPE[logits.dtype], t_idx.data_ptr(), t_val.data_ptr(), top, temperature,
+                            _vector(dloss, "dloss", n), scale, _vector(loss, "loss", n), _ptr(dlogits),
+                            0 if dlogits is None else _rows(dlogits, "dlogits", logits.dtype, (n, v)),
+                            _vector(dev_status, "dev_status", 1, torch.int32), _ptr(ws), nbytes, _stream())
+    _check(rc, "mlmc_distill")
+    return loss, dlogits
