@@ -8,10 +8,10 @@
 
 namespace mlmc {
 
-// C[i][j] = sum_c A(i, c) B(j, c), A(i, c) at a[i * a_i + c * a_c], likewise B.
+// C[i][j] = sum_c A(i, c) B(j, c).  An operand lies along the contraction (A(i, c) at a[i * lda + c]) or across it (at a[c * lda + i]).
 struct LinearArgs {
     const void *a, *b;
-    int64_t a_i, a_c, b_j, b_c, I, J, C;
+    int64_t lda, ldb, I, J, C;
     int act;
     const float* bias;     // forward: of column j
     const void* slope_z;   // dgrad: C is multiplied with act' of this
@@ -24,6 +24,10 @@ struct LinearArgs {
     int64_t ldo;
     int out_dtype;
     void* row_sum;         // wgrad: sum_c A(i, c), in out_dtype
+    int tiles_i, tiles_j;
+    int splits;            // the contraction is cut into this many parts, whose sums are joined by k_linear_join
+    int64_t split_len;     // entries of the contraction of a part, a multiple of a step's
+    float* part;           // [splits][I][J], then [splits][I] for row_sum
 };
 
 __device__ inline float act_value(float z, int act) {
@@ -41,51 +45,415 @@ __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
     else ((__bf16*)p)[at] = (__bf16)v;
 }
 
-constexpr int LIN_T = 64, LIN_C = 16;
 
-template <int DT> __global__ __launch_bounds__(256) void k_linear(LinearArgs g) {
-    __shared__ float sa[LIN_C][LIN_T + 1], sb[LIN_C][LIN_T + 1];
-    const int64_t i0 = (int64_t)blockIdx.y * LIN_T, j0 = (int64_t)blockIdx.x * LIN_T;
-    const int ti = (threadIdx.x >> 4) * 4, tj = (threadIdx.x & 15) * 4;
-    float acc[4][4] = {};
-    float sums = 0.f;
-    for (int64_t c0 = 0; c0 < g.C; c0 += LIN_C) {
-        for (int e = threadIdx.x; e < LIN_T * LIN_C; e += 256) {
-            // neighbouring threads along whichever index is contiguous
-            const int ic = g.a_c == 1 ? e % LIN_C : e / LIN_T, ii = g.a_c == 1 ? e / LIN_C : e % LIN_T;
-            const int jc = g.b_c == 1 ? e % LIN_C : e / LIN_T, jj = g.b_c == 1 ? e / LIN_C : e % LIN_T;
-            sa[ic][ii] = i0 + ii < g.I && c0 + ic < g.C ? to_f32(((const entry_t<DT>*)g.a)[(i0 + ii) * g.a_i + (c0 + ic) * g.a_c]) : 0.f;
-            sb[jc][jj] = j0 + jj < g.J && c0 + jc < g.C ? to_f32(((const entry_t<DT>*)g.b)[(j0 + jj) * g.b_j + (c0 + jc) * g.b_c]) : 0.f;
-        }
-        __syncthreads();
-        for (int c = 0; c < LIN_C; ++c)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(sa[c][ti + u], sb[c][tj + v], acc[u][v]);
-        if (g.row_sum && blockIdx.x == 0 && threadIdx.x < LIN_T)
-            for (int c = 0; c < LIN_C; ++c) sums += sa[c][threadIdx.x];
-        __syncthreads();
+using v4f = float __attribute__((ext_vector_type(4)));
+using v16f = float __attribute__((ext_vector_type(16)));
+using v8b = __bf16 __attribute__((ext_vector_type(8)));
+using v4s = short __attribute__((ext_vector_type(4)));
+using v8s = short __attribute__((ext_vector_type(8)));
+using chunk_t = int __attribute__((ext_vector_type(4)));                 // 16 bytes of a row
+using chunk_u = int __attribute__((ext_vector_type(4), aligned(2)));     // the same at any entry's place
+using lds_void = __attribute__((address_space(3))) void;
+using global_void = const __attribute__((address_space(1))) void;
+
+// 16 bytes of row `r`, columns c .. c + 16 / size - 1, of a matrix of R rows and C columns; zero outside.  A chunk that the row's end cuts is
+// taken from the row's last 16 bytes, shifted down: no branch, and the loads of several chunks are in flight together.  WIDE: rows have 16 bytes.
+template <int DT, bool WIDE> __device__ inline chunk_t chunk_or_zero(const void* p, int64_t ld, int64_t r, int64_t R, int64_t c, int64_t C) {
+    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
+    const entry_t<DT>* q = (const entry_t<DT>*)p + (r < R ? r : 0) * ld;
+    unsigned __int128 v = 0;
+    if (WIDE || C >= E) {
+        const int64_t at = c < C - E ? c : C - E;
+        v = __builtin_bit_cast(unsigned __int128, (chunk_t) * (const chunk_u*)(q + at));
+        const int64_t over = c - at;
+        v = over >= E || r >= R ? 0 : v >> (BITS * (int)over);
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < E; ++e)
+            if (r < R && c + e < C) v |= (unsigned __int128)(DT == MLMC_BF16 ? ((const uint16_t*)q)[c + e] : ((const uint32_t*)q)[c + e]) << (BITS * e);
     }
-    for (int u = 0; u < 4; ++u)
-        for (int v = 0; v < 4; ++v) {
-            const int64_t i = i0 + ti + u, j = j0 + tj + v;
-            if (i >= g.I || j >= g.J) continue;
-            float z = acc[u][v];
-            if (g.bias) z += g.bias[j];
-            if (g.z) store_as(g.z, i * g.ldz + j, DT, z);
-            z = g.slope_z ? z * act_slope(to_f32(((const entry_t<DT>*)g.slope_z)[i * g.ld_slope + j]), g.act) : act_value(z, g.act);
-            if (g.residual) z += to_f32(((const entry_t<DT>*)g.residual)[i * g.ldr + j]);
-            store_as(g.out, i * g.ldo + j, g.out_dtype, z);
-        }
-    if (g.row_sum && blockIdx.x == 0 && threadIdx.x < LIN_T && i0 + threadIdx.x < g.I) store_as(g.row_sum, i0 + threadIdx.x, g.out_dtype, sums);
+    return __builtin_bit_cast(chunk_t, v);
 }
 
-static mlmc_status linear_run(const LinearArgs& g, int dtype, hipStream_t st) {
-    const dim3 grid((unsigned)((g.J + LIN_T - 1) / LIN_T), (unsigned)((g.I + LIN_T - 1) / LIN_T));
-    if (dtype == MLMC_F32) MLMC_LAUNCH(K_LINEAR, st, (k_linear<MLMC_F32><<<grid, 256, 0, st>>>(g)));
-    else MLMC_LAUNCH(K_LINEAR, st, (k_linear<MLMC_BF16><<<grid, 256, 0, st>>>(g)));
+template <int DT> __device__ inline void load8(float (&v)[8], const void* p, int64_t at, int n) {
+    if constexpr (DT == MLMC_BF16) {
+        const __bf16* q = (const __bf16*)p + at;
+        if (n == 8) {
+            const v8b w = __builtin_bit_cast(v8b, (chunk_t) * (const chunk_u*)q);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
+        } else {
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)q[e] : 0.f;
+        }
+    } else {
+        const float* q = (const float*)p + at;
+        if (n == 8) {
+            const v4f w0 = __builtin_bit_cast(v4f, (chunk_t) * (const chunk_u*)q), w1 = __builtin_bit_cast(v4f, (chunk_t) * (const chunk_u*)(q + 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = w0[e]; v[4 + e] = w1[e]; }
+        } else {
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? q[e] : 0.f;
+        }
+    }
+}
+__device__ inline void store8(const float (&v)[8], void* p, int64_t at, int n, int dtype) {
+    if (n < 8) {
+        for (int e = 0; e < 8; ++e)
+            if (e < n) store_as(p, at + e, dtype, v[e]);
+    } else if (dtype == MLMC_BF16) {
+        v8b w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
+        *(chunk_u*)((__bf16*)p + at) = __builtin_bit_cast(chunk_t, w);
+    } else {
+        const v4f w0 = {v[0], v[1], v[2], v[3]}, w1 = {v[4], v[5], v[6], v[7]};
+        *(chunk_u*)((float*)p + at) = __builtin_bit_cast(chunk_t, w0);
+        *(chunk_u*)((float*)p + at + 4) = __builtin_bit_cast(chunk_t, w1);
+    }
+}
+
+// The epilogue of n <= 8 neighbouring entries of a row of the product.
+template <int DT> __device__ inline void epilogue8(const LinearArgs& g, int64_t i, int64_t j, float (&v)[8], int n) {
+    float u[8];
+    if (g.bias) {
+        load8<MLMC_F32>(u, g.bias, j, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += u[e];
+    }
+    if (g.z) store8(v, g.z, i * g.ldz + j, n, DT);
+    if (g.slope_z) {
+        load8<DT>(u, g.slope_z, i * g.ld_slope + j, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= act_slope(u[e], g.act);
+    } else if (g.act != MLMC_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_value(v[e], g.act);
+    }
+    if (g.residual) {
+        load8<DT>(u, g.residual, i * g.ldr + j, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += u[e];
+    }
+    store8(v, g.out, i * g.ldo + j, n, g.out_dtype);
+}
+
+// Where a step's operand lies in LDS, in 16-byte slots.  ALONG: a row of LDS is an index's 128 bytes of the contraction; else it is a
+// contraction index's T entries.  The slot in a row is exclusive-ored so that the lanes that read at once (eight rows' slots; or, transposing,
+// four rows' pairs of slots and the same eight rows below) lie in different banks.
+template <int DT, bool ALONG, int T> struct Lds {
+    static constexpr int E = DT == MLMC_BF16 ? 8 : 4, W = ALONG ? 8 : T / E;   // slots of a row
+    __device__ static int swizzle(int r) {
+        if (ALONG) return r & 7;
+        return DT == MLMC_BF16 ? ((r & 3) << 1) | (W >= 16 ? r & 8 : 0) : 0;
+    }
+    __device__ static int slot(int r, int c) { return r * W + (c ^ swizzle(r)); }
+};
+
+// Operand fragment of the matrix instructions for a quarter of a step: of index f * 32 + lane % 32 and, per half of the wave, 16 bytes of the
+// contraction.
+template <int DT, bool ALONG, int T> __device__ inline chunk_t fragment(const chunk_t* s, int f, int q) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (ALONG) {
+        return s[Lds<DT, true, T>::slot(f * 32 + (lane & 31), q * 2 + (lane >> 5))];
+    } else if constexpr (DT == MLMC_BF16) {
+        const int i = lane & 15, col = f * 32 + (lane & 16) + (i & 3) * 4, r = q * 16 + (lane >> 5) * 8 + (i >> 2);
+        v4s h[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const char* p = (const char*)(s + Lds<DT, false, T>::slot(r + 4 * k, col >> 3)) + ((col & 4) << 1);
+            h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+        }
+        return __builtin_bit_cast(chunk_t, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const float* p = (const float*)s;
+        v4f v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[(q * 8 + (lane >> 5) * 4 + k) * T + f * 32 + (lane & 31)];
+        return __builtin_bit_cast(chunk_t, v);
+    }
+}
+
+template <int DT> __device__ inline v16f multiply(chunk_t a, chunk_t b, v16f c) {
+    if constexpr (DT == MLMC_BF16) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+    } else {
+        const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k], y[k], c, 0, 0, 0);
+        return c;
+    }
+}
+
+template <int DT> __device__ inline float chunk_sum(chunk_t a) {
+    float s = 0.f;
+    if constexpr (DT == MLMC_BF16) {
+        const v8b v = __builtin_bit_cast(v8b, a);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += (float)v[e];
+    } else {
+        const v4f v = __builtin_bit_cast(v4f, a);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += v[e];
+    }
+    return s;
+}
+
+// One operand's way from memory to LDS: 128 bytes of the contraction (a step) for T indices, by NT threads.
+template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
+    static constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 8 * E, N = T * 8 / NT;   // N: chunks a thread moves
+    const void* p;
+    int64_t ld, i0, I, C;
+    unsigned off[N];   // byte offsets from the tile's base
+
+    using L = Lds<DT, ALONG, T>;
+    __device__ static int row(int q) { return q / L::W; }
+    __device__ static int chunk(int q) { return (q % L::W) ^ L::swizzle(q / L::W); }   // which chunk of the row slot q holds
+    __device__ void init(const void* p_, int64_t ld_, int64_t i0_, int64_t I_, int64_t C_) {
+        p = p_; ld = ld_; i0 = i0_; I = I_; C = C_;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int q = u * NT + threadIdx.x, r = row(q), c = chunk(q) * E;
+            // what lies past the matrix repeats its last entries: it reaches only results that are not stored
+            if (ALONG) off[u] = (unsigned)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
+            else off[u] = (unsigned)((r * ld + (i0 + c < I ? c : I - E - i0)) * (16 / E));
+        }
+    }
+    // a whole step, straight into LDS; `c` the first contraction index
+    __device__ void fetch(chunk_t* s, int64_t c) const {
+        const char* base = (const char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            __builtin_amdgcn_global_load_lds((global_void*)(base + off[u]), (lds_void*)(s + u * NT + (threadIdx.x & ~63)), 16, 0, 0);
+    }
+    // any step, by way of registers, zeros outside
+    __device__ void load(chunk_t (&v)[N], int64_t c) const {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int q = u * NT + threadIdx.x;
+            if (ALONG) v[u] = chunk_or_zero<DT, WIDE>(p, ld, i0 + row(q), I, c + chunk(q) * E, C);
+            else v[u] = chunk_or_zero<DT, WIDE>(p, ld, c + row(q), C, i0 + chunk(q) * E, I);
+        }
+    }
+    __device__ static void store(chunk_t* s, const chunk_t (&v)[N]) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) s[u * NT + threadIdx.x] = v[u];
+    }
+};
+
+// A tile of the product.  WM x WN waves, each FM x FN matrix instructions of 32 x 32.  AA, BA: the contraction is contiguous in A, B.
+// FAST: whole steps come straight into LDS.
+template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST>
+__global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
+    constexpr int NT = WM * WN * 64, TM = WM * FM * 32, TN = WN * FN * 32;
+    __shared__ chunk_t a0[TM * 8], b0[TN * 8], a1[TM * 8], b1[TN * 8];
+    using OpA = Operand<DT, AA, TM, NT, FAST>;
+    using OpB = Operand<DT, BA, TN, NT, FAST>;
+    constexpr int STEP = OpA::STEP;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
+    // neighbouring tiles to the workgroups of one die (workgroups go round the 8 dies), eight tile rows at a time
+    int t = blockIdx.x;
+    {
+        const int n = gridDim.x, q = n / 8, r = n % 8, x = t & 7;
+        t = x * q + (x < r ? x : r) + (t >> 3);
+    }
+    const int tiles = g.tiles_i * g.tiles_j, split = t / tiles;
+    t -= split * tiles;
+    const int band = t / (8 * g.tiles_j), in_band = t - band * 8 * g.tiles_j, high = min(8, g.tiles_i - band * 8);
+    const int ti = band * 8 + in_band % high, tj = in_band / high;
+    const int64_t i0 = (int64_t)ti * TM, j0 = (int64_t)tj * TN, c_begin = split * g.split_len, c_end = min(g.C, c_begin + g.split_len);
+    OpA A;
+    OpB B;
+    A.init(g.a, g.lda, i0, g.I, g.C);
+    B.init(g.b, g.ldb, j0, g.J, g.C);
+
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
+    float sums[FM] = {};
+    const bool rows = !AA && g.row_sum && tj == 0;   // this workgroup adds up A's entries; wave wn takes quarter wn of every step
+
+    const auto compute = [&](const chunk_t* sa, const chunk_t* sb) {
+        chunk_t fa[2][FM], fb[2][FN];
+        const auto read = [&](int q) {
+#pragma unroll
+            for (int m = 0; m < FM; ++m) fa[q & 1][m] = fragment<DT, AA, TM>(sa, wm * FM + m, q);
+#pragma unroll
+            for (int n = 0; n < FN; ++n) fb[q & 1][n] = fragment<DT, BA, TN>(sb, wn * FN + n, q);
+        };
+        read(0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {   // a quarter's fragments come while the one before is multiplied
+            if (q < 3) read(q + 1);
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!AA && rows) {
+            for (int q = wn; q < 4; q += WN)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) sums[m] += chunk_sum<DT>(fragment<DT, AA, TM>(sa, wm * FM + m, q));
+        }
+    };
+    const auto guarded = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
+        chunk_t va[OpA::N], vb[OpB::N];
+        A.load(va, c);
+        B.load(vb, c);
+        A.store(sa, va);
+        B.store(sb, vb);
+    };
+    const auto fetch = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
+        A.fetch(sa, c);
+        B.fetch(sb, c);
+    };
+    const auto arrived = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): also what goes to LDS by itself
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // the step at c from one pair of buffers while the next one comes into the other
+    const int64_t c_whole = FAST ? c_end - (c_end - c_begin) % STEP : c_end;
+    const auto step = [&](int64_t c, const chunk_t* sa, const chunk_t* sb, chunk_t* na, chunk_t* nb) {
+        if constexpr (FAST) {
+            if (c + STEP < c_whole) fetch(c + STEP, na, nb);
+            compute(sa, sb);
+        } else {
+            chunk_t va[OpA::N], vb[OpB::N];
+            A.load(va, c + STEP);
+            B.load(vb, c + STEP);
+            compute(sa, sb);
+            A.store(na, va);
+            B.store(nb, vb);
+        }
+        arrived();
+    };
+    if (c_begin < c_whole) {
+        if (FAST) fetch(c_begin, a0, b0);
+        else guarded(c_begin, a0, b0);
+        arrived();
+    }
+    int64_t c = c_begin;
+    for (; c + STEP < c_whole; c += 2 * STEP) {
+        step(c, a0, b0, a1, b1);
+        step(c + STEP, a1, b1, a0, b0);
+    }
+    if (c < c_whole) step(c, a0, b0, a1, b1);
+    if (c_whole < c_end) {
+        guarded(c_whole, a0, b0);
+        arrived();
+        compute(a0, b0);
+        arrived();
+    }
+
+    if (!AA && rows) {   // the halves of a wave, then the waves of a row of waves
+        float* s = (float*)b0;
+#pragma unroll
+        for (int m = 0; m < FM; ++m) {
+            const float v = sums[m] + __shfl_xor(sums[m], 32);
+            if (lane < 32) s[wn * TM + (wm * FM + m) * 32 + lane] = v;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < TM; i += NT) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < WN; ++w) v += s[w * TM + i];
+            if (i0 + i < g.I) {
+                if (g.splits > 1) g.part[(int64_t)g.splits * g.I * g.J + split * g.I + i0 + i] = v;
+                else store_as(g.row_sum, i0 + i, g.out_dtype, v);
+            }
+        }
+    }
+    // A wave's results 32 rows at a time through its own LDS, so that a lane has neighbouring entries of a row: a register of the matrix instruction holds
+    // four of them, which would store 32 bytes of a row at a time.
+    constexpr int WJ = FN * 32, SLOTS = WJ / 4;
+    chunk_t* stage = (wave < WM * WN / 2 ? a0 : a1) + (wave % (WM * WN / 2)) * 32 * SLOTS;
+    static_assert(WM * WN / 2 * 32 * SLOTS <= TM * 8, "half the waves' results fit in one buffer");
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const v4f v = {acc[m][n][4 * r], acc[m][n][4 * r + 1], acc[m][n][4 * r + 2], acc[m][n][4 * r + 3]};
+                const int slot = n * 8 + r * 2 + (lane >> 5), i = lane & 31;
+                stage[i * SLOTS + (slot ^ (i & 7))] = __builtin_bit_cast(chunk_t, v);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int p = 0; p < WJ / 16; ++p) {
+            constexpr int PER = WJ / 8;   // lanes of a row
+            const int i = p * (64 / PER) + lane / PER, c = lane % PER;
+            const v4f v0 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c) ^ (i & 7))]), v1 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c + 1) ^ (i & 7))]);
+            float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            const int64_t oi = i0 + (wm * FM + m) * 32 + i, oj = j0 + wn * WJ + c * 8;
+            if (oi < g.I && oj < g.J) {
+                const int n = (int)min((int64_t)8, g.J - oj);
+                if (g.splits > 1) store8(v, g.part, ((int64_t)split * g.I + oi) * g.J + oj, n, MLMC_F32);
+                else epilogue8<DT>(g, oi, oj, v, n);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+// The sums of the contraction's parts, in their order, and the epilogue.
+template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArgs g) {
+    const int64_t per_row = (g.J + 7) / 8, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t >= g.I * per_row) {
+        const int64_t i = t - g.I * per_row;
+        if (g.row_sum && i < g.I) {
+            float v = 0.f;
+            for (int s = 0; s < g.splits; ++s) v += g.part[(int64_t)g.splits * g.I * g.J + s * g.I + i];
+            store_as(g.row_sum, i, g.out_dtype, v);
+        }
+        return;
+    }
+    const int64_t i = t / per_row, j = (t - i * per_row) * 8;
+    const int n = (int)min((int64_t)8, g.J - j);
+    float v[8] = {};
+    for (int s = 0; s < g.splits; ++s) {
+        float u[8];
+        load8<MLMC_F32>(u, g.part, ((int64_t)s * g.I + i) * g.J + j, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += u[e];
+    }
+    epilogue8<DT>(g, i, j, v, n);
+}
+
+template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
+    constexpr int TM = WM * FM * 32, TN = WN * FN * 32;
+    g.tiles_i = (int)((g.I + TM - 1) / TM);
+    g.tiles_j = (int)((g.J + TN - 1) / TN);
+    const unsigned grid = (unsigned)((int64_t)g.tiles_i * g.tiles_j * g.splits);
+    MLMC_LAUNCH(K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, FAST><<<grid, WM * WN * 64, 0, st>>>(g)));
     return MLMC_OK;
+}
+
+// Whether whole steps of an operand may come straight into LDS: 16-byte chunks that are aligned and lie inside the matrix or outside, offsets within a tile that fit 32 bits.
+static bool operand_fast(const void* p, int64_t ld, int64_t width, int esize) {
+    const int E = 16 / esize;
+    return (uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0 && ld <= ((int64_t)1 << 22) / esize;
+}
+
+template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs g, hipStream_t st) {
+    constexpr int esize = DT == MLMC_BF16 ? 2 : 4;
+    const bool fast = operand_fast(g.a, g.lda, AA ? g.C : g.I, esize) && operand_fast(g.b, g.ldb, BA ? g.C : g.J, esize);
+    g.splits = 1;
+    g.split_len = g.C;
+    if (!fast) return launch_tile<DT, 2, 2, 2, 2, AA, BA, false>(g, st);
+    if constexpr (DT == MLMC_BF16)
+        if (((g.I + 255) / 256) * ((g.J + 255) / 256) >= 128) return launch_tile<DT, 2, 4, 4, 2, AA, BA, true>(g, st);
+    return launch_tile<DT, 2, 2, 2, 2, AA, BA, true>(g, st);
+}
+
+template <bool AA, bool BA> static mlmc_status linear_run(const LinearArgs& g, int dtype, hipStream_t st) {
+    return dtype == MLMC_F32 ? linear_layout<MLMC_F32, AA, BA>(g, st) : linear_layout<MLMC_BF16, AA, BA>(g, st);
 }
 
 constexpr int64_t LINEAR_ROWS_MAX = (int64_t)1 << 21;   // workgroups of 64 rows along the grid's second axis: under 2^16
@@ -116,9 +484,9 @@ mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t 
     const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
     if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
-    g.a = x; g.a_i = ldx; g.a_c = 1; g.b = weight; g.b_j = ldw; g.b_c = 1; g.I = rows; g.J = outputs; g.C = inputs;
+    g.a = x; g.lda = ldx; g.b = weight; g.ldb = ldw; g.I = rows; g.J = outputs; g.C = inputs;
     g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype;
-    return linear_run(g, dtype, (hipStream_t)hip_stream);
+    return linear_run<true, true>(g, dtype, (hipStream_t)hip_stream);
 }
 
 mlmc_status mlmc_linear_dgrad(const void* dy, int64_t lddy, const void* weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs,
@@ -132,10 +500,10 @@ mlmc_status mlmc_linear_dgrad(const void* dy, int64_t lddy, const void* weight, 
     const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
     if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
-    g.a = dy; g.a_i = lddy; g.a_c = 1; g.b = weight; g.b_j = 1; g.b_c = ldw; g.I = rows; g.J = inputs; g.C = outputs;
+    g.a = dy; g.lda = lddy; g.b = weight; g.ldb = ldw; g.I = rows; g.J = inputs; g.C = outputs;
     g.act = act; g.slope_z = act != MLMC_ACT_NONE ? z : nullptr; g.ld_slope = ldz; g.residual = residual; g.ldr = ldr;
     g.out = dx; g.ldo = lddx; g.out_dtype = dtype;
-    return linear_run(g, dtype, (hipStream_t)hip_stream);
+    return linear_run<true, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
 mlmc_status mlmc_linear_wgrad(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
@@ -146,9 +514,9 @@ mlmc_status mlmc_linear_wgrad(const void* dy, int64_t lddy, const void* x, int64
     const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
     if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
-    g.a = dy; g.a_i = 1; g.a_c = lddy; g.b = x; g.b_j = 1; g.b_c = ldx; g.I = outputs; g.J = inputs; g.C = rows;
+    g.a = dy; g.lda = lddy; g.b = x; g.ldb = ldx; g.I = outputs; g.J = inputs; g.C = rows;
     g.act = MLMC_ACT_NONE; g.out = dweight; g.ldo = lddw; g.out_dtype = grad_dtype; g.row_sum = dbias;
-    return linear_run(g, dtype, (hipStream_t)hip_stream);
+    return linear_run<false, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"
