@@ -54,25 +54,24 @@ using v8s = short __attribute__((ext_vector_type(8)));
 using chunk_t = int __attribute__((ext_vector_type(4)));                 // 16 bytes of a row
 using chunk_u = int __attribute__((ext_vector_type(4), aligned(2)));     // the same at any entry's place
 using lds_void = __attribute__((address_space(3))) void;
-using global_void = const __attribute__((address_space(1))) void;
 
-// 16 bytes of row `r`, columns c .. c + 16 / size - 1, of a matrix of R rows and C columns; zero outside.  A chunk that the row's end cuts is
-// taken from the row's last 16 bytes, shifted down: no branch, and the loads of several chunks are in flight together.  WIDE: rows have 16 bytes.
-template <int DT, bool WIDE> __device__ inline chunk_t chunk_or_zero(const void* p, int64_t ld, int64_t r, int64_t R, int64_t c, int64_t C) {
+// 16 bytes of row `r`, columns c .. c + 16 / size - 1, of a matrix of R rows and C columns; zero outside, once cut_chunk has been over them.  A chunk
+// that the row's end cuts is taken from the row's last 16 bytes and shifted down later: no branch and no wait between the loads.  WIDE: rows
+// have 16 bytes.
+template <int DT, bool WIDE> __device__ inline chunk_t raw_chunk(const void* p, int64_t ld, int64_t r, int64_t R, int64_t c, int64_t C) {
     constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
-    const entry_t<DT>* q = (const entry_t<DT>*)p + (r < R ? r : 0) * ld;
+    const entry_t<DT>* q = (const entry_t<DT>*)p + (r < R ? r : R - 1) * ld;
+    if (WIDE || C >= E) return *(const chunk_u*)(q + (c < C - E ? c : C - E));
     unsigned __int128 v = 0;
-    if (WIDE || C >= E) {
-        const int64_t at = c < C - E ? c : C - E;
-        v = __builtin_bit_cast(unsigned __int128, (chunk_t) * (const chunk_u*)(q + at));
-        const int64_t over = c - at;
-        v = over >= E || r >= R ? 0 : v >> (BITS * (int)over);
-    } else {
 #pragma unroll 1
-        for (int e = 0; e < E; ++e)
-            if (r < R && c + e < C) v |= (unsigned __int128)(DT == MLMC_BF16 ? ((const uint16_t*)q)[c + e] : ((const uint32_t*)q)[c + e]) << (BITS * e);
-    }
+    for (int e = 0; e < C; ++e) v |= (unsigned __int128)(DT == MLMC_BF16 ? ((const uint16_t*)q)[e] : ((const uint32_t*)q)[e]) << (BITS * e);
     return __builtin_bit_cast(chunk_t, v);
+}
+template <int DT, bool WIDE> __device__ inline chunk_t cut_chunk(chunk_t w, int64_t r, int64_t R, int64_t c, int64_t C) {
+    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
+    const int64_t first = WIDE || C >= E ? C - E : 0, over = c < first ? 0 : c - first;
+    const unsigned __int128 v = __builtin_bit_cast(unsigned __int128, w);
+    return __builtin_bit_cast(chunk_t, over >= E || r >= R ? (unsigned __int128)0 : v >> (BITS * (int)over));
 }
 
 template <int DT> __device__ inline void load8(float (&v)[8], const void* p, int64_t at, int n) {
@@ -149,29 +148,41 @@ template <int DT, bool ALONG, int T> struct Lds {
     __device__ static int slot(int r, int c) { return r * W + (c ^ swizzle(r)); }
 };
 
-// Operand fragment of the matrix instructions for a quarter of a step: of index f * 32 + lane % 32 and, per half of the wave, 16 bytes of the
-// contraction.
-template <int DT, bool ALONG, int T> __device__ inline chunk_t fragment(const chunk_t* s, int f, int q) {
-    const int lane = threadIdx.x & 63;
-    if constexpr (ALONG) {
-        return s[Lds<DT, true, T>::slot(f * 32 + (lane & 31), q * 2 + (lane >> 5))];
-    } else if constexpr (DT == MLMC_BF16) {
-        const int i = lane & 15, col = f * 32 + (lane & 16) + (i & 3) * 4, r = q * 16 + (lane >> 5) * 8 + (i >> 2);
-        v4s h[2];
+// Operand fragments of the matrix instructions for a quarter q of a step: of index (f0 + f) * 32 + lane % 32 and, per half of the wave, 16 bytes of
+// the contraction.  The lane's places are kept; f or q, whichever the slots' exclusive-or does not reach, goes into the instruction's offset.
+template <int DT, bool ALONG, int T, int F> struct Fragments {
+    using L = Lds<DT, ALONG, T>;
+    static constexpr int N = ALONG ? 4 : DT == MLMC_BF16 ? F : 1;
+    int place[N];   // bytes
+    __device__ void init(int f0) {
+        const int lane = threadIdx.x & 63, half = lane >> 5, i = lane & 15;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const char* p = (const char*)(s + Lds<DT, false, T>::slot(r + 4 * k, col >> 3)) + ((col & 4) << 1);
-            h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+        for (int n = 0; n < N; ++n) {
+            if (ALONG) place[n] = L::slot(f0 * 32 + (lane & 31), n * 2 + half) * 16;
+            else if (DT == MLMC_BF16) {
+                const int col = (f0 + n) * 32 + (lane & 16) + (i & 3) * 4;
+                place[n] = L::slot(half * 8 + (i >> 2), col >> 3) * 16 + ((col & 4) << 1);
+            } else place[n] = (half * 4 * T + f0 * 32 + (lane & 31)) * 4;
         }
-        return __builtin_bit_cast(chunk_t, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-        const float* p = (const float*)s;
-        v4f v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = p[(q * 8 + (lane >> 5) * 4 + k) * T + f * 32 + (lane & 31)];
-        return __builtin_bit_cast(chunk_t, v);
     }
-}
+    __device__ chunk_t get(const chunk_t* s, int f, int q) const {
+        const char* p = (const char*)s;
+        if constexpr (ALONG) {
+            return *(const chunk_t*)(p + place[q] + f * 32 * 128);
+        } else if constexpr (DT == MLMC_BF16) {
+            v4s h[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + place[f] + (q * 16 + 4 * k) * T * 2));
+            return __builtin_bit_cast(chunk_t, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            v4f v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = *(const float*)(p + place[0] + ((q * 8 + k) * T + f * 32) * 4);
+            return __builtin_bit_cast(chunk_t, v);
+        }
+    }
+};
 
 template <int DT> __device__ inline v16f multiply(chunk_t a, chunk_t b, v16f c) {
     if constexpr (DT == MLMC_BF16) {
@@ -220,23 +231,30 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
     }
     // a whole step, straight into LDS; `c` the first contraction index
     __device__ void fetch(chunk_t* s, int64_t c) const {
-        const char* base = (const char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E);
+        // a buffer load and not a global one: behind the latter the compiler takes every wait for LDS reads to be one for all of them
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc((char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E), 0, -1, 0x00027000);
+        const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x) & ~63;
 #pragma unroll
         for (int u = 0; u < N; ++u)
-            __builtin_amdgcn_global_load_lds((global_void*)(base + off[u]), (lds_void*)(s + u * NT + (threadIdx.x & ~63)), 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, (int)off[u], 0, 0, 0);
     }
     // any step, by way of registers, zeros outside
     __device__ void load(chunk_t (&v)[N], int64_t c) const {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int q = u * NT + threadIdx.x;
-            if (ALONG) v[u] = chunk_or_zero<DT, WIDE>(p, ld, i0 + row(q), I, c + chunk(q) * E, C);
-            else v[u] = chunk_or_zero<DT, WIDE>(p, ld, c + row(q), C, i0 + chunk(q) * E, I);
+            if (ALONG) v[u] = raw_chunk<DT, WIDE>(p, ld, i0 + row(q), I, c + chunk(q) * E, C);
+            else v[u] = raw_chunk<DT, WIDE>(p, ld, c + row(q), C, i0 + chunk(q) * E, I);
         }
     }
-    __device__ static void store(chunk_t* s, const chunk_t (&v)[N]) {
+    __device__ void store(chunk_t* s, const chunk_t (&v)[N], int64_t c) const {
 #pragma unroll
-        for (int u = 0; u < N; ++u) s[u * NT + threadIdx.x] = v[u];
+        for (int u = 0; u < N; ++u) {
+            const int q = u * NT + threadIdx.x;
+            if (ALONG) s[q] = cut_chunk<DT, WIDE>(v[u], i0 + row(q), I, c + chunk(q) * E, C);
+            else s[q] = cut_chunk<DT, WIDE>(v[u], c + row(q), C, i0 + chunk(q) * E, I);
+        }
     }
 };
 
@@ -276,36 +294,30 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
     float sums[FM] = {};
     const bool rows = !AA && g.row_sum && tj == 0;   // this workgroup adds up A's entries; wave wn takes quarter wn of every step
 
-    const auto compute = [&](const chunk_t* sa, const chunk_t* sb) {
-        chunk_t fa[2][FM], fb[2][FN];
-        const auto read = [&](int q) {
+    Fragments<DT, AA, TM, FM> FA;
+    Fragments<DT, BA, TN, FN> FB;
+    FA.init(wm * FM);
+    FB.init(wn * FN);
+    chunk_t fa[2][FM], fb[2][FN];
+    const auto read = [&](const chunk_t* sa, const chunk_t* sb, int q) {
 #pragma unroll
-            for (int m = 0; m < FM; ++m) fa[q & 1][m] = fragment<DT, AA, TM>(sa, wm * FM + m, q);
+        for (int m = 0; m < FM; ++m) fa[q & 1][m] = FA.get(sa, m, q);
 #pragma unroll
-            for (int n = 0; n < FN; ++n) fb[q & 1][n] = fragment<DT, BA, TN>(sb, wn * FN + n, q);
-        };
-        read(0);
+        for (int n = 0; n < FN; ++n) fb[q & 1][n] = FB.get(sb, n, q);
+        __builtin_amdgcn_sched_barrier(0);   // else the reads sink behind the matrix instructions that they are to run under
+    };
+    const auto multiply_quarter = [&](int q) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {   // a quarter's fragments come while the one before is multiplied
-            if (q < 3) read(q + 1);
+        for (int m = 0; m < FM; ++m)
 #pragma unroll
-            for (int m = 0; m < FM; ++m)
-#pragma unroll
-                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (!AA && rows) {
+            for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto add_rows = [&](const chunk_t* sa) {
+        if (!AA && rows)
             for (int q = wn; q < 4; q += WN)
 #pragma unroll
-                for (int m = 0; m < FM; ++m) sums[m] += chunk_sum<DT>(fragment<DT, AA, TM>(sa, wm * FM + m, q));
-        }
-    };
-    const auto guarded = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
-        chunk_t va[OpA::N], vb[OpB::N];
-        A.load(va, c);
-        B.load(vb, c);
-        A.store(sa, va);
-        B.store(sb, vb);
+                for (int m = 0; m < FM; ++m) sums[m] += chunk_sum<DT>(FA.get(sa, m, q));
     };
     const auto fetch = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
         A.fetch(sa, c);
@@ -317,37 +329,61 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // the step at c from one pair of buffers while the next one comes into the other
+    // The step at c from one pair of buffers.  Fragments are read a quarter ahead of the matrix instructions; before the last quarter's the wave waits for the other
+    // pair to be full and for the others to have read this one, so that the next step's first fragments and the loads after next go out under it.
     const int64_t c_whole = FAST ? c_end - (c_end - c_begin) % STEP : c_end;
-    const auto step = [&](int64_t c, const chunk_t* sa, const chunk_t* sb, chunk_t* na, chunk_t* nb) {
-        if constexpr (FAST) {
-            if (c + STEP < c_whole) fetch(c + STEP, na, nb);
-            compute(sa, sb);
-        } else {
-            chunk_t va[OpA::N], vb[OpB::N];
+    const auto step = [&](int64_t c, chunk_t* sa, chunk_t* sb, chunk_t* na, chunk_t* nb) {
+        chunk_t va[OpA::N], vb[OpB::N];
+        if constexpr (!FAST) {
             A.load(va, c + STEP);
             B.load(vb, c + STEP);
-            compute(sa, sb);
-            A.store(na, va);
-            B.store(nb, vb);
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            read(sa, sb, q + 1);
+            multiply_quarter(q);
+        }
+        add_rows(sa);
+        if constexpr (!FAST) {
+            A.store(na, va, c + STEP);
+            B.store(nb, vb, c + STEP);
         }
         arrived();
+        if (FAST && c + 2 * STEP < c_whole) fetch(c + 2 * STEP, sa, sb);
+        read(na, nb, 0);
+        multiply_quarter(3);
+    };
+    const auto guarded = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
+        chunk_t va[OpA::N], vb[OpB::N];
+        A.load(va, c);
+        B.load(vb, c);
+        A.store(sa, va, c);
+        B.store(sb, vb, c);
     };
     if (c_begin < c_whole) {
-        if (FAST) fetch(c_begin, a0, b0);
+        if constexpr (FAST) fetch(c_begin, a0, b0);
         else guarded(c_begin, a0, b0);
         arrived();
+        if (FAST && c_begin + STEP < c_whole) fetch(c_begin + STEP, a1, b1);
+        read(a0, b0, 0);
+        int64_t c = c_begin;
+        for (; c + STEP < c_whole; c += 2 * STEP) {
+            step(c, a0, b0, a1, b1);
+            step(c + STEP, a1, b1, a0, b0);
+        }
+        if (c < c_whole) step(c, a0, b0, a1, b1);
+        arrived();
     }
-    int64_t c = c_begin;
-    for (; c + STEP < c_whole; c += 2 * STEP) {
-        step(c, a0, b0, a1, b1);
-        step(c + STEP, a1, b1, a0, b0);
-    }
-    if (c < c_whole) step(c, a0, b0, a1, b1);
-    if (c_whole < c_end) {
+    if (c_whole < c_end) {   // a step that is not whole
         guarded(c_whole, a0, b0);
         arrived();
-        compute(a0, b0);
+        read(a0, b0, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (q < 3) read(a0, b0, q + 1);
+            multiply_quarter(q);
+        }
+        add_rows(a0);
         arrived();
     }
 
