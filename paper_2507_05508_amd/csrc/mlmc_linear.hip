@@ -4,6 +4,8 @@
 //   forward:  z = x W^T + b, y = act(z) + r         x [n][k], W [m][k]; contraction over k
 //   dgrad:    dx = (dy W) act'(z) + r               dy [n][m];          contraction over m
 //   wgrad:    dW = dy^T x, db = sum over rows of dy;                    contraction over n
+#include <type_traits>
+
 #include "mlmc_worker.h"
 
 namespace mlmc {
@@ -26,19 +28,28 @@ struct LinearArgs {
     void* row_sum;         // wgrad: sum_c A(i, c), in out_dtype
     int tiles_i, tiles_j;
     int splits;            // the contraction is cut into this many parts, whose sums are joined by k_linear_join
-    int64_t split_len;     // entries of the contraction of a part, a multiple of a step's
+    int split_len;         // entries of the contraction of a part, a multiple of a step's
     float* part;           // [splits][I][J], then [splits][I] for row_sum
 };
 
-__device__ inline float act_value(float z, int act) {
-    if (act == MLMC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;   // a NaN stays one
-    if (act == MLMC_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    return z;
+// The tail of the normal distribution, Phi(-|z|) = erfc(|z| / sqrt 2) / 2, and its density's exponential e^(-z^2 / 2), which the slope of gelu needs as well.  erfc by
+// the rational approximation 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: off by at most 1.5e-7, half of which reaches Phi.
+__device__ inline float normal_tail(float z, float& e) {
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
+    const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    return 0.5f * p * t * e;
 }
-__device__ inline float act_slope(float z, int act) {
-    if (act == MLMC_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (act == MLMC_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
-    return 1.f;
+__device__ inline float relu(float z) { return z > 0.f || z != z ? z : 0.f; }   // a NaN stays one
+__device__ inline float gelu(float z) {
+    float e;
+    const float tail = normal_tail(z, e);
+    return z * (z > 0.f ? 1.0f - tail : tail);
+}
+__device__ inline float gelu_slope(float z) {
+    float e;
+    const float tail = normal_tail(z, e);
+    return fmaf(z * 0.39894228040143268f, e, z > 0.f ? 1.0f - tail : tail);
 }
 __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
     if (dtype == MLMC_F32) ((float*)p)[at] = v;
@@ -82,6 +93,7 @@ template <int DT> __device__ inline void load8(float (&v)[8], const void* p, int
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
         } else {
+#pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)q[e] : 0.f;
         }
     } else {
@@ -91,12 +103,14 @@ template <int DT> __device__ inline void load8(float (&v)[8], const void* p, int
 #pragma unroll
             for (int e = 0; e < 4; ++e) { v[e] = w0[e]; v[4 + e] = w1[e]; }
         } else {
+#pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = e < n ? q[e] : 0.f;
         }
     }
 }
 __device__ inline void store8(const float (&v)[8], void* p, int64_t at, int n, int dtype) {
     if (n < 8) {
+#pragma unroll
         for (int e = 0; e < 8; ++e)
             if (e < n) store_as(p, at + e, dtype, v[e]);
     } else if (dtype == MLMC_BF16) {
@@ -111,30 +125,43 @@ __device__ inline void store8(const float (&v)[8], void* p, int64_t at, int n, i
     }
 }
 
-// The epilogue of n <= 8 neighbouring entries of a row of the product.
-template <int DT> __device__ inline void epilogue8(const LinearArgs& g, int64_t i, int64_t j, float (&v)[8], int n) {
-    float u[8];
-    if (g.bias) {
-        load8<MLMC_F32>(u, g.bias, j, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += u[e];
+// The epilogue of n <= 8 neighbouring entries of a row of the product, cut in two so that the loads of several rows are in flight together.
+struct Epilogue {
+    float slope[8], residual[8];
+    template <int DT> __device__ void load(const LinearArgs& g, int64_t i, int64_t j, int n) {
+        if (g.slope_z) load8<DT>(slope, g.slope_z, i * g.ld_slope + j, n);
+        if (g.residual) load8<DT>(residual, g.residual, i * g.ldr + j, n);
     }
-    if (g.z) store8(v, g.z, i * g.ldz + j, n, DT);
-    if (g.slope_z) {
-        load8<DT>(u, g.slope_z, i * g.ld_slope + j, n);
+    template <int DT> __device__ void finish(const LinearArgs& g, int64_t i, int64_t j, float (&v)[8], const float (&bias)[8], int n) const {
+        if (g.bias) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= act_slope(u[e], g.act);
-    } else if (g.act != MLMC_ACT_NONE) {
+            for (int e = 0; e < 8; ++e) v[e] += bias[e];
+        }
+        if (g.z) store8(v, g.z, i * g.ldz + j, n, DT);
+        if (g.act == MLMC_ACT_GELU) {   // the branches outside of the loops: inside they took longer than the arithmetic
+            if (g.slope_z) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_value(v[e], g.act);
+                for (int e = 0; e < 8; ++e) v[e] *= gelu_slope(slope[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = gelu(v[e]);
+            }
+        } else if (g.act == MLMC_ACT_RELU) {
+            if (g.slope_z) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = slope[e] > 0.f ? v[e] : 0.f * v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = relu(v[e]);
+            }
+        }
+        if (g.residual) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += residual[e];
+        }
+        store8(v, g.out, i * g.ldo + j, n, g.out_dtype);
     }
-    if (g.residual) {
-        load8<DT>(u, g.residual, i * g.ldr + j, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += u[e];
-    }
-    store8(v, g.out, i * g.ldo + j, n, g.out_dtype);
-}
+};
 
 // Where a step's operand lies in LDS, in 16-byte slots.  ALONG: a row of LDS is an index's 128 bytes of the contraction; else it is a
 // contraction index's T entries.  The slot in a row is exclusive-ored so that the lanes that read at once (eight rows' slots; or, transposing,
@@ -229,11 +256,12 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
             else off[u] = (unsigned)((r * ld + (i0 + c < I ? c : I - E - i0)) * (16 / E));
         }
     }
-    // a whole step, straight into LDS; `c` the first contraction index
-    __device__ void fetch(chunk_t* s, int64_t c) const {
+    // a whole step, straight into LDS; `c` its first contraction index.  From `end` on nothing is read (the buffer has no entries, zeros arrive).
+    __device__ void fetch(chunk_t* s, int c, int end) const {
         // a buffer load and not a global one: behind the latter the compiler takes every wait for LDS reads to be one for all of them
         const __amdgpu_buffer_rsrc_t rsrc =
-            __builtin_amdgcn_make_buffer_rsrc((char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E), 0, -1, 0x00027000);
+            __builtin_amdgcn_make_buffer_rsrc((char*)p + (ALONG ? i0 * ld + c : (int64_t)c * ld + i0) * (16 / E), 0,
+                                              __builtin_amdgcn_readfirstlane(c < end ? -1 : 0) /* the select is compiled into a vector one */, 0x00027000);
         const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x) & ~63;
 #pragma unroll
         for (int u = 0; u < N; ++u)
@@ -274,11 +302,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         const int n = gridDim.x, q = n / 8, r = n % 8, x = t & 7;
         t = x * q + (x < r ? x : r) + (t >> 3);
     }
-    const int tiles = g.tiles_i * g.tiles_j, split = t / tiles;
+    // (divisions run on the vector unit; what follows from them is uniform, which the buffers' descriptors have to be)
+    const auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int tiles = g.tiles_i * g.tiles_j, split = uniform(t / tiles);
     t -= split * tiles;
-    const int band = t / (8 * g.tiles_j), in_band = t - band * 8 * g.tiles_j, high = min(8, g.tiles_i - band * 8);
-    const int ti = band * 8 + in_band % high, tj = in_band / high;
-    const int64_t i0 = (int64_t)ti * TM, j0 = (int64_t)tj * TN, c_begin = split * g.split_len, c_end = min(g.C, c_begin + g.split_len);
+    const int band = uniform(t / (8 * g.tiles_j)), in_band = t - band * 8 * g.tiles_j, high = min(8, g.tiles_i - band * 8);
+    const int tj = uniform(in_band / high), ti = band * 8 + in_band - tj * high;
+    const int64_t i0 = (int64_t)ti * TM, j0 = (int64_t)tj * TN;
+    const int C = (int)g.C, c_begin = split * g.split_len, c_end = min(C, c_begin + g.split_len);   // at most 2^21
     OpA A;
     OpB B;
     A.init(g.a, g.lda, i0, g.I, g.C);
@@ -304,13 +335,20 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         for (int m = 0; m < FM; ++m) fa[q & 1][m] = FA.get(sa, m, q);
 #pragma unroll
         for (int n = 0; n < FN; ++n) fb[q & 1][n] = FB.get(sb, n, q);
-        __builtin_amdgcn_sched_barrier(0);   // else the reads sink behind the matrix instructions that they are to run under
     };
     const auto multiply_quarter = [&](int q) {
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
             for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
+        // the reads (and, in the last quarter, the loads) between the matrix instructions: left alone they sink behind them
+        constexpr int PRODUCTS = FM * FN * (DT == MLMC_BF16 ? 1 : 4), READS = FM * (AA ? 1 : DT == MLMC_BF16 ? 2 : 4) + FN * (BA ? 1 : DT == MLMC_BF16 ? 2 : 4);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (FAST && q == 3) __builtin_amdgcn_sched_group_barrier(0x10, (OpA::N + OpB::N + READS - 1) / READS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, (PRODUCTS + READS - 1) / READS, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto add_rows = [&](const chunk_t* sa) {
@@ -318,10 +356,6 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
             for (int q = wn; q < 4; q += WN)
 #pragma unroll
                 for (int m = 0; m < FM; ++m) sums[m] += chunk_sum<DT>(FA.get(sa, m, q));
-    };
-    const auto fetch = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
-        A.fetch(sa, c);
-        B.fetch(sb, c);
     };
     const auto arrived = [&] {
         asm volatile("" ::: "memory");
@@ -331,8 +365,13 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
     };
     // The step at c from one pair of buffers.  Fragments are read a quarter ahead of the matrix instructions; before the last quarter's the wave waits for the other
     // pair to be full and for the others to have read this one, so that the next step's first fragments and the loads after next go out under it.
-    const int64_t c_whole = FAST ? c_end - (c_end - c_begin) % STEP : c_end;
-    const auto step = [&](int64_t c, chunk_t* sa, chunk_t* sb, chunk_t* na, chunk_t* nb) {
+    // (no branch around the loads: it would keep them from between the matrix instructions)
+    const int c_whole = FAST ? c_end - (c_end - c_begin) % STEP : c_end;
+    const auto fetch = [&](int c, chunk_t* sa, chunk_t* sb) {
+        A.fetch(sa, c, c_whole);
+        B.fetch(sb, c, c_whole);
+    };
+    const auto step = [&](int c, chunk_t* sa, chunk_t* sb, chunk_t* na, chunk_t* nb) {
         chunk_t va[OpA::N], vb[OpB::N];
         if constexpr (!FAST) {
             A.load(va, c + STEP);
@@ -349,11 +388,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
             B.store(nb, vb, c + STEP);
         }
         arrived();
-        if (FAST && c + 2 * STEP < c_whole) fetch(c + 2 * STEP, sa, sb);
+        if constexpr (FAST) fetch(c + 2 * STEP, sa, sb);
         read(na, nb, 0);
         multiply_quarter(3);
     };
-    const auto guarded = [&](int64_t c, chunk_t* sa, chunk_t* sb) {
+    const auto guarded = [&](int c, chunk_t* sa, chunk_t* sb) {
         chunk_t va[OpA::N], vb[OpB::N];
         A.load(va, c);
         B.load(vb, c);
@@ -364,9 +403,9 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         if constexpr (FAST) fetch(c_begin, a0, b0);
         else guarded(c_begin, a0, b0);
         arrived();
-        if (FAST && c_begin + STEP < c_whole) fetch(c_begin + STEP, a1, b1);
+        if constexpr (FAST) fetch(c_begin + STEP, a1, b1);
         read(a0, b0, 0);
-        int64_t c = c_begin;
+        int c = c_begin;
         for (; c + STEP < c_whole; c += 2 * STEP) {
             step(c, a0, b0, a1, b1);
             step(c + STEP, a1, b1, a0, b0);
@@ -410,29 +449,55 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
     constexpr int WJ = FN * 32, SLOTS = WJ / 4;
     chunk_t* stage = (wave < WM * WN / 2 ? a0 : a1) + (wave % (WM * WN / 2)) * 32 * SLOTS;
     static_assert(WM * WN / 2 * 32 * SLOTS <= TM * 8, "half the waves' results fit in one buffer");
-#pragma unroll
-    for (int m = 0; m < FM; ++m) {
-#pragma unroll
-        for (int n = 0; n < FN; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const v4f v = {acc[m][n][4 * r], acc[m][n][4 * r + 1], acc[m][n][4 * r + 2], acc[m][n][4 * r + 3]};
-                const int slot = n * 8 + r * 2 + (lane >> 5), i = lane & 31;
-                stage[i * SLOTS + (slot ^ (i & 7))] = __builtin_bit_cast(chunk_t, v);
-            }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int PER = WJ / 8;   // lanes of a row
+    const int c8 = lane % PER;
+    const int64_t oj = j0 + wn * WJ + c8 * 8;
+    const int n8 = (int)max((int64_t)0, min((int64_t)8, g.J - oj));
+    float bias[8];
+    if (g.bias && n8 > 0) load8<MLMC_F32>(bias, g.bias, oj, n8);
 #pragma unroll 1
-        for (int p = 0; p < WJ / 16; ++p) {
-            constexpr int PER = WJ / 8;   // lanes of a row
-            const int i = p * (64 / PER) + lane / PER, c = lane % PER;
-            const v4f v0 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c) ^ (i & 7))]), v1 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c + 1) ^ (i & 7))]);
-            float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            const int64_t oi = i0 + (wm * FM + m) * 32 + i, oj = j0 + wn * WJ + c * 8;
-            if (oi < g.I && oj < g.J) {
-                const int n = (int)min((int64_t)8, g.J - oj);
-                if (g.splits > 1) store8(v, g.part, ((int64_t)split * g.I + oi) * g.J + oj, n, MLMC_F32);
-                else epilogue8<DT>(g, oi, oj, v, n);
+    for (int mm = 0; mm < FM; ++mm) {   // not unrolled: what follows the stores is long
+        const int64_t im = i0 + (wm * FM + mm) * 32;
+#pragma unroll
+        for (int m = 0; m < FM; ++m) {
+            if (m != mm) continue;
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const v4f v = {acc[m][n][4 * r], acc[m][n][4 * r + 1], acc[m][n][4 * r + 2], acc[m][n][4 * r + 3]};
+                    const int slot = n * 8 + r * 2 + (lane >> 5), i = lane & 31;
+                    stage[i * SLOTS + (slot ^ (i & 7))] = __builtin_bit_cast(chunk_t, v);
+                }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const auto rows_of = [&](int p, auto batch, auto cut) __attribute__((always_inline)) {
+            constexpr int K = decltype(batch)::value;
+            const int n = decltype(cut)::value ? n8 : 8;
+            float v[K][8];
+            Epilogue ep[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int i = (p + k) * (64 / PER) + lane / PER;
+                const v4f v0 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c8) ^ (i & 7))]), v1 = __builtin_bit_cast(v4f, stage[i * SLOTS + ((2 * c8 + 1) ^ (i & 7))]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[k][e] = v0[e]; v[k][4 + e] = v1[e]; }
+                if (g.splits == 1 && im + i < g.I && n8 > 0) ep[k].template load<DT>(g, im + i, oj, n);
             }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int64_t oi = im + (p + k) * (64 / PER) + lane / PER;
+                if (oi >= g.I || n8 <= 0) continue;
+                if (g.splits > 1) store8(v[k], g.part, ((int64_t)split * g.I + oi) * g.J + oj, n, MLMC_F32);
+                else ep[k].template finish<DT>(g, oi, oj, v[k], bias, n);
+            }
+        };
+        if (j0 + TN <= g.J) {
+#pragma unroll 1
+            for (int p = 0; p < WJ / 16; p += 4) rows_of(p, std::integral_constant<int, 4>{}, std::false_type{});
+        } else {
+#pragma unroll 1
+            for (int p = 0; p < WJ / 16; ++p) rows_of(p, std::integral_constant<int, 1>{}, std::true_type{});
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -459,7 +524,11 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArg
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += u[e];
     }
-    epilogue8<DT>(g, i, j, v, n);
+    float bias[8];
+    if (g.bias) load8<MLMC_F32>(bias, g.bias, j, n);
+    Epilogue ep;
+    ep.load<DT>(g, i, j, n);
+    ep.finish<DT>(g, i, j, v, bias, n);
 }
 
 template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
@@ -481,10 +550,10 @@ template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs 
     constexpr int esize = DT == MLMC_BF16 ? 2 : 4;
     const bool fast = operand_fast(g.a, g.lda, AA ? g.C : g.I, esize) && operand_fast(g.b, g.ldb, BA ? g.C : g.J, esize);
     g.splits = 1;
-    g.split_len = g.C;
+    g.split_len = (int)g.C;
     if (!fast) return launch_tile<DT, 2, 2, 2, 2, AA, BA, false>(g, st);
     if constexpr (DT == MLMC_BF16)
-        if (((g.I + 255) / 256) * ((g.J + 255) / 256) >= 128) return launch_tile<DT, 2, 4, 4, 2, AA, BA, true>(g, st);
+        if (((g.I + 255) / 256) * ((g.J + 255) / 256) >= 128) return launch_tile<DT, 2, 2, 4, 4, AA, BA, true>(g, st);
     return launch_tile<DT, 2, 2, 2, 2, AA, BA, true>(g, st);
 }
 
