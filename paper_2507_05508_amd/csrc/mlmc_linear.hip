@@ -170,7 +170,7 @@ template <int DT, bool ALONG, int T> struct Lds {
     static constexpr int E = DT == MLMC_BF16 ? 8 : 4, W = ALONG ? 8 : T / E;   // slots of a row
     __device__ static int swizzle(int r) {
         if (ALONG) return r & 7;
-        return DT == MLMC_BF16 ? ((r & 3) << 1) | (W >= 16 ? r & 8 : 0) : 0;
+        return DT == MLMC_BF16 ? (((r & 3) << 1) | (r & 8)) & (W - 1) : 0;
     }
     __device__ static int slot(int r, int c) { return r * W + (c ^ swizzle(r)); }
 };
@@ -241,7 +241,8 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
     static constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 8 * E, N = T * 8 / NT;   // N: chunks a thread moves
     const void* p;
     int64_t ld, i0, I, C;
-    unsigned off[N];   // byte offsets from the tile's base
+    using off_t = std::conditional_t<WIDE, unsigned, int64_t>;
+    off_t off[N];   // byte offsets from the tile's base
 
     using L = Lds<DT, ALONG, T>;
     __device__ static int row(int q) { return q / L::W; }
@@ -252,8 +253,8 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
         for (int u = 0; u < N; ++u) {
             const int q = u * NT + threadIdx.x, r = row(q), c = chunk(q) * E;
             // what lies past the matrix repeats its last entries: it reaches only results that are not stored
-            if (ALONG) off[u] = (unsigned)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
-            else off[u] = (unsigned)((r * ld + (i0 + c < I ? c : I - E - i0)) * (16 / E));
+            if (ALONG) off[u] = (off_t)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
+            else off[u] = (off_t)((r * ld + (i0 + c < I || I < E ? c : I - E - i0)) * (16 / E));
         }
     }
     // a whole step, straight into LDS; `c` its first contraction index.  From `end` on nothing is read (the buffer has no entries, zeros arrive).
@@ -268,7 +269,14 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, (int)off[u], 0, 0, 0);
     }
     // any step, by way of registers, zeros outside
+    __device__ bool inside(int64_t c) const { return c + STEP <= C && (ALONG || i0 + T <= I); }
     __device__ void load(chunk_t (&v)[N], int64_t c) const {
+        if (inside(c)) {
+            const char* base = (const char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E);
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[u] = *(const chunk_u*)(base + off[u]);
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int q = u * NT + threadIdx.x;
@@ -277,6 +285,11 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
         }
     }
     __device__ void store(chunk_t* s, const chunk_t (&v)[N], int64_t c) const {
+        if (inside(c)) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) s[u * NT + threadIdx.x] = v[u];
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int q = u * NT + threadIdx.x;
@@ -341,13 +354,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         for (int m = 0; m < FM; ++m)
 #pragma unroll
             for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
-        // the reads (and, in the last quarter, the loads) between the matrix instructions: left alone they sink behind them
-        constexpr int PRODUCTS = FM * FN * (DT == MLMC_BF16 ? 1 : 4), READS = FM * (AA ? 1 : DT == MLMC_BF16 ? 2 : 4) + FN * (BA ? 1 : DT == MLMC_BF16 ? 2 : 4);
+        // the reads and the loads between the matrix instructions: left alone they sink behind them
+        constexpr int READS = FM * (AA ? 1 : DT == MLMC_BF16 ? 2 : 4) + FN * (BA ? 1 : DT == MLMC_BF16 ? 2 : 4);
 #pragma unroll
         for (int i = 0; i < READS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            if (FAST && q == 3) __builtin_amdgcn_sched_group_barrier(0x10, (OpA::N + OpB::N + READS - 1) / READS, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, (PRODUCTS + READS - 1) / READS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            if (FAST && (q == 3 || q == 0)) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -364,13 +378,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         asm volatile("" ::: "memory");
     };
     // The step at c from one pair of buffers.  Fragments are read a quarter ahead of the matrix instructions; before the last quarter's the wave waits for the other
-    // pair to be full and for the others to have read this one, so that the next step's first fragments and the loads after next go out under it.
-    // (no branch around the loads: it would keep them from between the matrix instructions)
+    // pair to be full and for the others to have read this one, so that the next step's first fragments go out under it.  The step after next comes into the
+    // pair that this frees, A's part under the last quarter, B's under the next step's first: a CU takes in 16 bytes a lane at 4 lanes a clock, and all
+    // of a step's loads at once hold up the matrix instructions behind them (8192 x 4096 x 4096: 250 us, spread 235).  No branch around the loads: it would
+    // keep them from between the matrix instructions.
     const int c_whole = FAST ? c_end - (c_end - c_begin) % STEP : c_end;
-    const auto fetch = [&](int c, chunk_t* sa, chunk_t* sb) {
-        A.fetch(sa, c, c_whole);
-        B.fetch(sb, c, c_whole);
-    };
     const auto step = [&](int c, chunk_t* sa, chunk_t* sb, chunk_t* na, chunk_t* nb) {
         chunk_t va[OpA::N], vb[OpB::N];
         if constexpr (!FAST) {
@@ -380,6 +392,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             read(sa, sb, q + 1);
+            if (FAST && q == 0) B.fetch(nb, c + STEP, c_whole);
             multiply_quarter(q);
         }
         add_rows(sa);
@@ -388,7 +401,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
             B.store(nb, vb, c + STEP);
         }
         arrived();
-        if constexpr (FAST) fetch(c + 2 * STEP, sa, sb);
+        if constexpr (FAST) A.fetch(sa, c + 2 * STEP, c_whole);
         read(na, nb, 0);
         multiply_quarter(3);
     };
@@ -400,10 +413,12 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         B.store(sb, vb, c);
     };
     if (c_begin < c_whole) {
-        if constexpr (FAST) fetch(c_begin, a0, b0);
-        else guarded(c_begin, a0, b0);
+        if constexpr (FAST) {
+            A.fetch(a0, c_begin, c_whole);
+            B.fetch(b0, c_begin, c_whole);
+        } else guarded(c_begin, a0, b0);
         arrived();
-        if constexpr (FAST) fetch(c_begin + STEP, a1, b1);
+        if constexpr (FAST) A.fetch(a1, c_begin + STEP, c_whole);
         read(a0, b0, 0);
         int c = c_begin;
         for (; c + STEP < c_whole; c += 2 * STEP) {
@@ -443,13 +458,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
                 else store_as(g.row_sum, i0 + i, g.out_dtype, v);
             }
         }
+        __syncthreads();
     }
     // A wave's results 32 rows at a time through its own LDS, so that a lane has neighbouring entries of a row: a register of the matrix instruction holds
     // four of them, which would store 32 bytes of a row at a time.
     constexpr int WJ = FN * 32, SLOTS = WJ / 4;
-    chunk_t* stage = (wave < WM * WN / 2 ? a0 : a1) + (wave % (WM * WN / 2)) * 32 * SLOTS;
-    static_assert(WM * WN / 2 * 32 * SLOTS <= TM * 8, "half the waves' results fit in one buffer");
+    static_assert(WM * WN / 2 * 32 * SLOTS <= (TM > TN ? TM : TN) * 8, "half the waves' results fit in one buffer");
+    chunk_t* stage = (wave < WM * WN / 2 ? (TM > TN ? a0 : b0) : (TM > TN ? a1 : b1)) + (wave % (WM * WN / 2)) * 32 * SLOTS;
     constexpr int PER = WJ / 8;   // lanes of a row
+    constexpr int BATCH = FM * FN >= 8 || WJ < 64 ? 2 : 4;   // the large tile's registers are full of results
     const int c8 = lane % PER;
     const int64_t oj = j0 + wn * WJ + c8 * 8;
     const int n8 = (int)max((int64_t)0, min((int64_t)8, g.J - oj));
@@ -494,7 +511,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         };
         if (j0 + TN <= g.J) {
 #pragma unroll 1
-            for (int p = 0; p < WJ / 16; p += 4) rows_of(p, std::integral_constant<int, 4>{}, std::false_type{});
+            for (int p = 0; p < WJ / 16; p += BATCH) rows_of(p, std::integral_constant<int, BATCH>{}, std::false_type{});
         } else {
 #pragma unroll 1
             for (int p = 0; p < WJ / 16; ++p) rows_of(p, std::integral_constant<int, 1>{}, std::true_type{});
@@ -531,12 +548,49 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArg
     ep.finish<DT>(g, i, j, v, bias, n);
 }
 
+// The tiles: rows and columns, microseconds of a step of a tile that has a CU to itself, and of everything else of a launch.
+enum LinearTile { TILE_32 = 0, TILE_64, TILE_128, TILE_256, TILES };
+struct TileCost { int rows, cols; float step_us[2], other_us; };   // [dtype]
+constexpr TileCost tile_costs[TILES] = {{32, 128, {0.60f, 0.30f}, 6.f}, {64, 128, {1.0f, 0.35f}, 7.f}, {128, 128, {1.9f, 0.55f}, 8.f}, {256, 256, {0.f, 1.25f}, 16.f}};
+constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
+
+struct LinearPlan { int tile, splits, split_len; };
+
+// The tile and the number of parts of the contraction that the costs above say to be the fastest: tiles come in rounds of one for every CU, a part more
+// makes the rounds finer and the join longer.
+static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool fast) {
+    const int step = dtype == MLMC_BF16 ? 64 : 32;
+    const int64_t steps = (C + step - 1) / step;
+    LinearPlan best = {TILE_128, 1, (int)C};
+    float least = 3.0e38f;
+    for (int t = 0; t < TILES; ++t) {
+        if (t == TILE_256 && (dtype != MLMC_BF16 || !fast)) continue;
+        const TileCost& k = tile_costs[t];
+        const int64_t tiles = ((I + k.rows - 1) / k.rows) * ((J + k.cols - 1) / k.cols);
+        for (int s = 1; s <= SPLITS_MAX && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
+            const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
+            if (parts != s) continue;
+            const float us = k.other_us * (t == TILE_256 ? (float)rounds : 1.f) + (float)(rounds * len) * k.step_us[dtype] + (s > 1 ? 4.f + 2.0e-6f * (float)(s * I) * (float)J : 0.f);
+            if (us < least) {
+                least = us;
+                best = {t, s, (int)(len * step)};
+            }
+        }
+    }
+    return best;
+}
+static size_t linear_part_bytes(const LinearPlan& p, int64_t I, int64_t J) { return p.splits > 1 ? (size_t)p.splits * (size_t)(I * J + I) * sizeof(float) : 0; }
+
 template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
     constexpr int TM = WM * FM * 32, TN = WN * FN * 32;
     g.tiles_i = (int)((g.I + TM - 1) / TM);
     g.tiles_j = (int)((g.J + TN - 1) / TN);
     const unsigned grid = (unsigned)((int64_t)g.tiles_i * g.tiles_j * g.splits);
     MLMC_LAUNCH(K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, FAST><<<grid, WM * WN * 64, 0, st>>>(g)));
+    if (g.splits > 1) {
+        const unsigned groups = (unsigned)((g.I * ((g.J + 7) / 8) + g.I + 255) / 256);
+        MLMC_LAUNCH(K_LINEAR_JOIN, st, (k_linear_join<DT><<<groups, 256, 0, st>>>(g)));
+    }
     return MLMC_OK;
 }
 
@@ -546,15 +600,21 @@ static bool operand_fast(const void* p, int64_t ld, int64_t width, int esize) {
     return (uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0 && ld <= ((int64_t)1 << 22) / esize;
 }
 
+template <int DT, bool AA, bool BA, bool FAST> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
+    if constexpr (DT == MLMC_BF16 && FAST)
+        if (tile == TILE_256) return launch_tile<DT, 2, 4, 4, 2, AA, BA, FAST>(g, st);
+    if (tile == TILE_128) return launch_tile<DT, 2, 2, 2, 2, AA, BA, FAST>(g, st);
+    if (tile == TILE_64) return launch_tile<DT, 1, 4, 2, 1, AA, BA, FAST>(g, st);
+    return launch_tile<DT, 1, 4, 1, 1, AA, BA, FAST>(g, st);
+}
+
 template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs g, hipStream_t st) {
     constexpr int esize = DT == MLMC_BF16 ? 2 : 4;
     const bool fast = operand_fast(g.a, g.lda, AA ? g.C : g.I, esize) && operand_fast(g.b, g.ldb, BA ? g.C : g.J, esize);
-    g.splits = 1;
-    g.split_len = (int)g.C;
-    if (!fast) return launch_tile<DT, 2, 2, 2, 2, AA, BA, false>(g, st);
-    if constexpr (DT == MLMC_BF16)
-        if (((g.I + 255) / 256) * ((g.J + 255) / 256) >= 128) return launch_tile<DT, 2, 2, 4, 4, AA, BA, true>(g, st);
-    return launch_tile<DT, 2, 2, 2, 2, AA, BA, true>(g, st);
+    const LinearPlan p = linear_plan(g.I, g.J, g.C, DT, fast);
+    g.splits = p.splits;
+    g.split_len = p.split_len;
+    return fast ? linear_tile<DT, AA, BA, true>(g, p.tile, st) : linear_tile<DT, AA, BA, false>(g, p.tile, st);
 }
 
 template <bool AA, bool BA> static mlmc_status linear_run(const LinearArgs& g, int dtype, hipStream_t st) {
@@ -574,8 +634,16 @@ using namespace mlmc;
 extern "C" {
 
 size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs) {
-    (void)rows; (void)outputs; (void)inputs;
-    return 0;
+    if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0) return 0;
+    const int64_t size[3][3] = {{rows, outputs, inputs}, {rows, inputs, outputs}, {outputs, inputs, rows}};
+    size_t most = 0;
+    for (const auto& z : size)
+        for (int dtype : {MLMC_F32, MLMC_BF16})
+            for (int fast = 0; fast < (dtype == MLMC_BF16 ? 2 : 1); ++fast) {   // 32-bit entries have the same tiles either way
+                const size_t need = linear_part_bytes(linear_plan(z[0], z[1], z[2], dtype, fast), z[0], z[1]);
+                most = need > most ? need : most;
+            }
+    return most;
 }
 
 mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
@@ -590,7 +658,7 @@ mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t 
     if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
     g.a = x; g.lda = ldx; g.b = weight; g.ldb = ldw; g.I = rows; g.J = outputs; g.C = inputs;
-    g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype;
+    g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype; g.part = (float*)ws;
     return linear_run<true, true>(g, dtype, (hipStream_t)hip_stream);
 }
 
@@ -607,7 +675,7 @@ mlmc_status mlmc_linear_dgrad(const void* dy, int64_t lddy, const void* weight, 
     LinearArgs g = {};
     g.a = dy; g.lda = lddy; g.b = weight; g.ldb = ldw; g.I = rows; g.J = inputs; g.C = outputs;
     g.act = act; g.slope_z = act != MLMC_ACT_NONE ? z : nullptr; g.ld_slope = ldz; g.residual = residual; g.ldr = ldr;
-    g.out = dx; g.ldo = lddx; g.out_dtype = dtype;
+    g.out = dx; g.ldo = lddx; g.out_dtype = dtype; g.part = (float*)ws;
     return linear_run<true, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
@@ -620,7 +688,7 @@ mlmc_status mlmc_linear_wgrad(const void* dy, int64_t lddy, const void* x, int64
     if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
     g.a = dy; g.lda = lddy; g.b = x; g.ldb = ldx; g.I = outputs; g.J = inputs; g.C = rows;
-    g.act = MLMC_ACT_NONE; g.out = dweight; g.ldo = lddw; g.out_dtype = grad_dtype; g.row_sum = dbias;
+    g.act = MLMC_ACT_NONE; g.out = dweight; g.ldo = lddw; g.out_dtype = grad_dtype; g.row_sum = dbias; g.part = (float*)ws;
     return linear_run<false, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
