@@ -548,10 +548,79 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArg
     ep.finish<DT>(g, i, j, v, bias, n);
 }
 
-// The tiles: rows and columns, microseconds of a step of a tile that has a CU to itself, and of everything else of a launch.
+// The forward product of up to 16 rows: bound by reading the weight once.  A workgroup has 16 outputs, its waves share the contraction and each has many
+// 16-byte loads in flight, straight into the registers of the matrix instructions (16 x 16): no LDS, no second launch.  One row of 4096 x 4096 bf16: 33.6 MB.
+constexpr int FEW_ROWS = 16, FEW_WAVES = 8, FEW_DEPTH = 8;
+template <int DT, bool WIDE> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs g) {
+    constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 4 * E;   // entries of the contraction a load of a wave covers, 64 bytes of each of 16 rows
+    __shared__ float part[FEW_WAVES][FEW_ROWS][FEW_ROWS + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, chunk = lane >> 4;
+    const int64_t j0 = (int64_t)blockIdx.x * 16, jr = min(j0 + r, g.J - 1);
+    const bool row = r < g.I;
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+    const auto product = [&](chunk_t w, chunk_t x) {
+        if constexpr (DT == MLMC_BF16) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, w), __builtin_bit_cast(v8b, x), acc, 0, 0, 0);
+        } else {
+            const v4f u = __builtin_bit_cast(v4f, w), v = __builtin_bit_cast(v4f, x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[k], v[k], acc, 0, 0, 0);
+        }
+    };
+    const char* pw = (const char*)((const entry_t<DT>*)g.b + jr * g.ldb + chunk * E);
+    const char* px = (const char*)((const entry_t<DT>*)g.a + (row ? r : 0) * g.lda + chunk * E);
+    const int C = (int)g.C, whole = C / STEP;   // C is at most 2^21
+    constexpr chunk_t zero = {0, 0, 0, 0};
+    for (int s = wave; s < whole; s += FEW_WAVES * FEW_DEPTH) {
+        chunk_t w[FEW_DEPTH], x[FEW_DEPTH];
+#pragma unroll
+        for (int u = 0; u < FEW_DEPTH; ++u) {
+            const int at = s + u * FEW_WAVES;
+            const bool in = at < whole;
+            w[u] = in ? (chunk_t) * (const chunk_u*)(pw + (int64_t)at * 64) : zero;
+            x[u] = in && row ? (chunk_t) * (const chunk_u*)(px + (int64_t)at * 64) : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < FEW_DEPTH; ++u) product(w[u], x[u]);
+    }
+    if (wave == FEW_WAVES - 1 && whole * STEP < C) {   // the rest
+        const int64_t c = whole * STEP + chunk * E;
+        const chunk_t w = cut_chunk<DT, WIDE>(raw_chunk<DT, WIDE>(g.b, g.ldb, jr, g.J, c, C), jr, g.J, c, C);
+        const chunk_t x = cut_chunk<DT, WIDE>(raw_chunk<DT, WIDE>(g.a, g.lda, r, g.I, c, C), r, g.I, c, C);
+        product(w, x);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][r][chunk * 4 + k] = acc[k];
+    __syncthreads();
+    const int64_t i = threadIdx.x >> 4, j = j0 + (threadIdx.x & 15);
+    if (threadIdx.x >= 256 || i >= g.I || j >= g.J) return;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) v += part[w][i][threadIdx.x & 15];
+    if (g.bias) v += g.bias[j];
+    if (g.z) store_as(g.z, i * g.ldz + j, DT, v);
+    if (g.act == MLMC_ACT_GELU) v = gelu(v);
+    else if (g.act == MLMC_ACT_RELU) v = relu(v);
+    if (g.residual) v += to_f32(((const entry_t<DT>*)g.residual)[i * g.ldr + j]);
+    store_as(g.out, i * g.ldo + j, DT, v);
+}
+
+template <int DT> static mlmc_status linear_few(const LinearArgs& g, hipStream_t st) {
+    const unsigned grid = (unsigned)((g.J + 15) / 16);
+    if (g.C >= (DT == MLMC_BF16 ? 8 : 4)) MLMC_LAUNCH(K_LINEAR_FEW, st, (k_linear_few<DT, true><<<grid, FEW_WAVES * 64, 0, st>>>(g)));
+    else MLMC_LAUNCH(K_LINEAR_FEW, st, (k_linear_few<DT, false><<<grid, FEW_WAVES * 64, 0, st>>>(g)));
+    return MLMC_OK;
+}
+
+// The tiles: rows and columns; microseconds of a step of a tile that has a CU to itself, of one among others, of the beginning and end of a round of tiles.
+// Fitted to sweeps of tiles and parts, microseconds of the best of either side: 2048 x 2048 x 2048 bf16, tiles 32 / 64 / 128 / 256: 34 / 25 / 28 / 43; 4096 x 1024 over
+// 8192: 166 / 97 / 84 (2 parts) / 83 (4); 1 x 4096 x 4096: 13.1 (8 parts) / 13.5 / 14.1 / 20.5; 4096 x 4096 x 512: 39 / 34 / 32 / 28; 200 x 8192 x 2048: 20 / 22 / 23 / 31;
+// fp32 512 x 512 over 8192: 43 (8) / 43 (8) / 47 (16); 1000 x 2049 x 1537: 91 (2) / 87 (4) / 86 (3); 2048 x 2048 x 2048: 139 / 129 / 126.
 enum LinearTile { TILE_32 = 0, TILE_64, TILE_128, TILE_256, TILES };
-struct TileCost { int rows, cols; float step_us[2], other_us; };   // [dtype]
-constexpr TileCost tile_costs[TILES] = {{32, 128, {0.60f, 0.30f}, 6.f}, {64, 128, {1.0f, 0.35f}, 7.f}, {128, 128, {1.9f, 0.55f}, 8.f}, {256, 256, {0.f, 1.25f}, 16.f}};
+struct TileCost { int rows, cols; float alone_us[2], among_us[2], round_us; };   // [dtype]
+constexpr TileCost tile_costs[TILES] = {{32, 128, {0.55f, 0.42f}, {0.53f, 0.28f}, 0.7f}, {64, 128, {0.95f, 0.44f}, {0.95f, 0.33f}, 1.3f},
+                                        {128, 128, {1.85f, 0.70f}, {1.85f, 0.50f}, 2.5f}, {256, 256, {0.f, 1.50f}, {0.f, 1.60f}, 11.f}};
+constexpr float LAUNCH_US = 5.f, JOIN_US = 3.f, JOIN_ENTRY_US = 1.6e-6f;
 constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
 
 struct LinearPlan { int tile, splits, split_len; };
@@ -570,7 +639,8 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
         for (int s = 1; s <= SPLITS_MAX && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
             const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
             if (parts != s) continue;
-            const float us = k.other_us * (t == TILE_256 ? (float)rounds : 1.f) + (float)(rounds * len) * k.step_us[dtype] + (s > 1 ? 4.f + 2.0e-6f * (float)(s * I) * (float)J : 0.f);
+            const float us = LAUNCH_US + (float)rounds * (k.round_us + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[dtype]) +
+                             (s > 1 ? JOIN_US + JOIN_ENTRY_US * (float)(s * I) * (float)J : 0.f);
             if (us < least) {
                 least = us;
                 best = {t, s, (int)(len * step)};
@@ -659,6 +729,7 @@ mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t 
     LinearArgs g = {};
     g.a = x; g.lda = ldx; g.b = weight; g.ldb = ldw; g.I = rows; g.J = outputs; g.C = inputs;
     g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype; g.part = (float*)ws;
+    if (rows <= FEW_ROWS) return dtype == MLMC_F32 ? linear_few<MLMC_F32>(g, (hipStream_t)hip_stream) : linear_few<MLMC_BF16>(g, (hipStream_t)hip_stream);
     return linear_run<true, true>(g, dtype, (hipStream_t)hip_stream);
 }
 
