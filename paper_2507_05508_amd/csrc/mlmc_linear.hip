@@ -57,33 +57,9 @@ __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
 }
 
 
-using v4f = float __attribute__((ext_vector_type(4)));
 using v16f = float __attribute__((ext_vector_type(16)));
-using v8b = __bf16 __attribute__((ext_vector_type(8)));
 using v4s = short __attribute__((ext_vector_type(4)));
-using v8s = short __attribute__((ext_vector_type(8)));
-using chunk_t = int __attribute__((ext_vector_type(4)));                 // 16 bytes of a row
-using chunk_u = int __attribute__((ext_vector_type(4), aligned(2)));     // the same at any entry's place
 using lds_void = __attribute__((address_space(3))) void;
-
-// 16 bytes of row `r`, columns c .. c + 16 / size - 1, of a matrix of R rows and C columns; zero outside, once cut_chunk has been over them.  A chunk
-// that the row's end cuts is taken from the row's last 16 bytes and shifted down later: no branch and no wait between the loads.  WIDE: rows
-// have 16 bytes.
-template <int DT, bool WIDE> __device__ inline chunk_t raw_chunk(const void* p, int64_t ld, int64_t r, int64_t R, int64_t c, int64_t C) {
-    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
-    const entry_t<DT>* q = (const entry_t<DT>*)p + (r < R ? r : R - 1) * ld;
-    if (WIDE || C >= E) return *(const chunk_u*)(q + (c < C - E ? c : C - E));
-    unsigned __int128 v = 0;
-#pragma unroll 1
-    for (int e = 0; e < C; ++e) v |= (unsigned __int128)(DT == MLMC_BF16 ? ((const uint16_t*)q)[e] : ((const uint32_t*)q)[e]) << (BITS * e);
-    return __builtin_bit_cast(chunk_t, v);
-}
-template <int DT, bool WIDE> __device__ inline chunk_t cut_chunk(chunk_t w, int64_t r, int64_t R, int64_t c, int64_t C) {
-    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
-    const int64_t first = WIDE || C >= E ? C - E : 0, over = c < first ? 0 : c - first;
-    const unsigned __int128 v = __builtin_bit_cast(unsigned __int128, w);
-    return __builtin_bit_cast(chunk_t, over >= E || r >= R ? (unsigned __int128)0 : v >> (BITS * (int)over));
-}
 
 template <int DT> __device__ inline void load8(float (&v)[8], const void* p, int64_t at, int n) {
     if constexpr (DT == MLMC_BF16) {

@@ -20,10 +20,216 @@ struct NormArgs {
     int64_t ldy, lddx;
     float* stats;
     float* part;          // [groups][2][d] sums of a group's rows
-    int64_t groups;       // workgroups, each takes rows group, group + groups, ...
+    int64_t groups;
     void *dweight, *dbias;
     int grad_dtype;
 };
+
+// ---- rows that fit in the registers of T threads, P entries each ------------------------------------------------------
+
+// A thread's N chunks of 16 bytes of a row, T threads side by side; zeros from column d >= 8 on.  A row's base is uniform over a wave, so that an address is one
+// register.  A chunk that the row's end cuts is the row's last 16 bytes, shifted down.
+template <int DT, int T, int P> struct RowChunks {
+    static constexpr int E = DT == MLMC_BF16 ? 8 : 4, N = P / E, BYTES = 16 / E;
+    int d, col0;
+    __device__ RowChunks(int64_t d_, int t) : d((int)d_), col0(t * E) {}
+    __device__ int col(int n) const { return col0 + n * T * E; }
+    __device__ void load(chunk_t (&v)[N], const void* row) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = *(const chunk_u*)((const char*)row + (unsigned)(min(col(n), d - E) * BYTES));
+    }
+    __device__ void to_floats(float (&f)[P], const chunk_t (&v)[N]) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            chunk_t c = v[n];
+            const int over = col(n) - (d - E);
+            if (over > 0) c = over >= E ? chunk_t{0, 0, 0, 0} : __builtin_bit_cast(chunk_t, __builtin_bit_cast(unsigned __int128, c) >> (over * BYTES * 8));
+            if constexpr (DT == MLMC_BF16) {
+                const v8b u = __builtin_bit_cast(v8b, c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[n * E + e] = (float)u[e];
+            } else {
+                const v4f u = __builtin_bit_cast(v4f, c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[n * E + e] = u[e];
+            }
+        }
+    }
+    __device__ void store(void* row, const float (&f)[P]) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            char* q = (char*)row + (unsigned)(col(n) * BYTES);
+            if (col(n) + E <= d) {
+                entry_t<DT> __attribute__((ext_vector_type(E))) u;
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] = (entry_t<DT>)f[n * E + e];
+                *(chunk_u*)q = __builtin_bit_cast(chunk_t, u);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col(n) + e < d) ((entry_t<DT>*)q)[e] = (entry_t<DT>)f[n * E + e];
+            }
+        }
+    }
+    // zero from column d on
+    __device__ void cut(float (&f)[P]) const {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (col(n) + E > d) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[n * E + e] = col(n) + e < d ? f[n * E + e] : 0.f;
+            }
+    }
+    // column of entry e of the thread
+    __device__ int at(int e) const { return col(e / E) + e % E; }
+};
+
+// Sums of two values over the T threads of a row; `part`: LDS that no earlier round may still be reading.
+template <int T> __device__ inline void row_sums(float& a, float& b, float2* part) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if (T == 64) return;
+    const int first = threadIdx.x / T * (T / 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll 4
+    for (int w = 0; w < T / 64; ++w) {
+        const float2 v = part[first + w];
+        a += v.x;
+        b += v.y;
+    }
+}
+
+// 1 / sqrt v: the instruction where it is exact to an ulp, which leaves out subnormal numbers
+__device__ inline float inverse_root(float v) { return v >= 1.2e-38f ? __builtin_amdgcn_rsqf(v) : 1.0f / sqrtf(v); }
+
+// A workgroup takes WG / T rows at a time, and weight and bias stay in registers from round to round.  The next round's rows are on their way while one is worked on.
+template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG, P <= 8 ? 8 : 4) void k_norm_forward_rows(NormArgs a) {
+    using Row = RowChunks<DT, T, P>;
+    constexpr int R = WG / T;
+    __shared__ float2 part[2][2][WG / 64];
+    const Row of(a.d, threadIdx.x % T);
+    float w[P], b[P];
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        const int j = of.at(e);
+        w[e] = a.weight && j < of.d ? a.weight[j] : 1.0f;
+        b[e] = a.bias && j < of.d ? a.bias[j] : 0.0f;
+    }
+    const float inv_d = 1.0f / (float)a.d;
+    chunk_t next[Row::N];
+    const auto fetch = [&](int64_t row) { of.load(next, (const entry_t<DT>*)a.x + (row < a.rows ? row : a.rows - 1) * a.ldx); };
+    int64_t row = (int64_t)blockIdx.x * R + __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+    fetch(row);
+    int odd = 0;
+    for (int64_t base = (int64_t)blockIdx.x * R; base < a.rows; base += (int64_t)gridDim.x * R, row += (int64_t)gridDim.x * R, odd ^= 1) {
+        float x[P], s = 0.f, q = 0.f, none = 0.f;
+        of.to_floats(x, next);
+        fetch(row + (int64_t)gridDim.x * R);
+#pragma unroll
+        for (int e = 0; e < P; ++e) s += x[e];
+        row_sums<T>(s, none, part[odd][0]);
+        const float mean = s * inv_d;
+#pragma unroll
+        for (int e = 0; e < P; ++e) x[e] -= mean;
+        of.cut(x);
+#pragma unroll
+        for (int e = 0; e < P; ++e) q = fmaf(x[e], x[e], q);
+        row_sums<T>(q, none, part[odd][1]);
+        const float rstd = inverse_root(fmaf(q, inv_d, a.eps));
+        if (row >= a.rows) continue;
+#pragma unroll
+        for (int e = 0; e < P; ++e) x[e] = fmaf(x[e] * rstd, w[e], b[e]);
+        of.store((entry_t<DT>*)a.y + row * a.ldy, x);
+        if (a.stats && threadIdx.x % T == 0) *(float2*)(a.stats + 2 * row) = make_float2(mean, rstd);
+    }
+}
+
+// The same for the gradient: x and dy are read once, a thread's columns of dweight and dbias are added up in its registers over all its rows, then over the workgroup's rows
+// in LDS, and a workgroup leaves one partial sum of each for k_norm_join.
+template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG) void k_norm_backward_rows(NormArgs a) {
+    constexpr bool AHEAD = P <= 8;   // the next round's rows on their way: with 16 entries a thread there are no registers for them
+    using Row = RowChunks<DT, T, P>;
+    constexpr int R = WG / T;
+    __shared__ float2 part[2][WG / 64];
+    __shared__ float add[R > 1 ? 2 * T * P : 1];
+    const int t = threadIdx.x % T, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+    const Row of(a.d, t);
+    float w[P], dw[P] = {}, db[P] = {};
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        const int j = of.at(e);
+        w[e] = a.weight && j < of.d ? a.weight[j] : 1.0f;
+    }
+    const float inv_d = 1.0f / (float)a.d;
+    chunk_t nx[Row::N], ny[Row::N];
+    float2 ns;
+    const auto fetch = [&](int64_t row) {
+        row = row < a.rows ? row : a.rows - 1;
+        of.load(nx, (const entry_t<DT>*)a.x + row * a.ldx);
+        of.load(ny, (const entry_t<DT>*)a.dy + row * a.lddy);
+        ns = make_float2(a.stats_in[2 * row], a.stats_in[2 * row + 1]);
+    };
+    int64_t row = (int64_t)blockIdx.x * R + sub;
+    if (AHEAD) fetch(row);
+    int odd = 0;
+    for (int64_t base = (int64_t)blockIdx.x * R; base < a.rows; base += a.groups * R, row += a.groups * R, odd ^= 1) {
+        if (!AHEAD) fetch(row);
+        float h[P], c[P], s = 0.f, q = 0.f;
+        const float mean = ns.x, rstd = ns.y;
+        of.to_floats(h, nx);
+        of.to_floats(c, ny);
+        if (R > 1 && row >= a.rows) {   // the last round's rows that are not there
+#pragma unroll
+            for (int e = 0; e < P; ++e) c[e] = 0.f;
+        }
+        if (AHEAD) fetch(row + a.groups * R);
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            h[e] = (h[e] - mean) * rstd;
+            dw[e] = fmaf(c[e], h[e], dw[e]);   // past column d dy is zero
+            db[e] += c[e];
+            c[e] *= w[e];
+            s += c[e];
+            q = fmaf(c[e], h[e], q);
+        }
+        row_sums<T>(s, q, part[odd]);
+        if (row >= a.rows) continue;
+        s *= inv_d;
+        q *= inv_d;
+#pragma unroll
+        for (int e = 0; e < P; ++e) c[e] = rstd * (fmaf(-h[e], q, c[e]) - s);
+        of.store((entry_t<DT>*)a.dx + row * a.lddx, c);
+    }
+    if (!a.part) return;
+    if constexpr (R > 1) {   // the sub-rows' sums one after the other
+        for (int r = 0; r < R; ++r) {
+            if (sub == r) {
+#pragma unroll
+                for (int e = 0; e < P; ++e) {   // thread-major: a wave's lanes side by side
+                    float* p = add + 2 * e * T + t;
+                    if (r == 0) { p[0] = dw[e]; p[T] = db[e]; }
+                    else if (r < R - 1) { p[0] += dw[e]; p[T] += db[e]; }
+                    else { dw[e] += p[0]; db[e] += p[T]; }
+                }
+            }
+            __syncthreads();
+        }
+        if (sub != R - 1) return;
+    }
+    float* p = a.part + 2 * (int64_t)blockIdx.x * a.d;
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        const int j = of.at(e);
+        if (j < of.d) {
+            p[j] = dw[e];
+            p[of.d + j] = db[e];
+        }
+    }
+}
+
+// ---- wider rows, and those of less than 16 bytes ----------------------------------------------------------------------------------------------------
 
 // One workgroup per row, which it reads three times; the second and third read come from the caches.
 template <int DT> __global__ __launch_bounds__(NORM_WG) void k_norm_forward(NormArgs a) {
@@ -85,30 +291,79 @@ template <int DT> __global__ __launch_bounds__(NORM_WG) void k_norm_columns(Norm
     a.part[(2 * (int64_t)blockIdx.y + 1) * a.d + j] = db;
 }
 
-// The groups' sums of a column, in the order of the groups.
-__global__ __launch_bounds__(NORM_WG) void k_norm_join(NormArgs a) {
-    const int64_t j = (int64_t)blockIdx.x * NORM_WG + threadIdx.x;
-    if (j >= a.d) return;
-    float dw = 0.f, db = 0.f;
-    for (int64_t g = 0; g < a.groups; ++g) {
-        dw += a.part[(2 * g) * a.d + j];
-        db += a.part[(2 * g + 1) * a.d + j];
+// The groups' sums: a lane has a column, the 16 waves take the groups in turn and their sums are added in the waves' order.
+constexpr int JOIN_WAVES = 16;
+__global__ __launch_bounds__(JOIN_WAVES * 64) void k_norm_join(NormArgs a) {
+    __shared__ float sum[JOIN_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = blockIdx.y;   // 0: dweight, 1: dbias
+    void* out = which ? a.dbias : a.dweight;
+    if (!out) return;
+    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+    float v = 0.f;
+    if (j < a.d) {
+#pragma unroll 8
+        for (int64_t g = wave; g < a.groups; g += JOIN_WAVES) v += a.part[(2 * g + which) * a.d + j];
     }
-    if (a.grad_dtype == MLMC_F32) {
-        if (a.dweight) ((float*)a.dweight)[j] = dw;
-        if (a.dbias) ((float*)a.dbias)[j] = db;
-    } else {
-        if (a.dweight) ((__bf16*)a.dweight)[j] = (__bf16)dw;
-        if (a.dbias) ((__bf16*)a.dbias)[j] = (__bf16)db;
-    }
+    sum[wave][lane] = v;
+    __syncthreads();
+    if (wave || j >= a.d) return;
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < JOIN_WAVES; ++w) v += sum[w][lane];
+    if (a.grad_dtype == MLMC_F32) ((float*)out)[j] = v;
+    else ((__bf16*)out)[j] = (__bf16)v;
 }
 
+constexpr int64_t NORM_ROW_MIN = 8, NORM_ROW_MAX = 16384;   // widths of the rows that are kept in registers
+static int row_threads(int64_t d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }   // 8 entries each, 16 from 8192 on
+
+// Workgroups of the backward pass, of 1024 threads, each of which leaves a partial sum of every column: one for every CU (its registers are full then), fewer if there are not the rows.
 static int64_t norm_groups(int64_t rows, int64_t d) {
-    (void)d;
-    return rows < 64 ? rows : 64;
+    if (d < NORM_ROW_MIN || d > NORM_ROW_MAX) return rows < 64 ? rows : 64;
+    const int64_t at_once = 1024 / row_threads(d), groups = (rows + at_once - 1) / at_once;
+    return groups < 256 ? groups : 256;
 }
 
 static bool norm_sizes_ok(int64_t rows, int64_t d) { return rows >= 0 && rows < ((int64_t)1 << 31) && d >= 1 && d < ((int64_t)1 << 31); }
+
+template <int DT, int T, int P> static mlmc_status forward_rows(const NormArgs& a, hipStream_t st) {
+    constexpr int WG = T < 256 ? 256 : T, R = WG / T;
+    const int64_t all = (a.rows + R - 1) / R, most = 256 * ((P <= 8 ? 2048 : 1024) / WG);   // as many as are on the chip at once
+    MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward_rows<DT, T, P, WG><<<(unsigned)(all < most ? all : most), WG, 0, st>>>(a)));
+    return MLMC_OK;
+}
+template <int DT> static mlmc_status norm_forward(const NormArgs& a, hipStream_t st) {
+    if (a.d < NORM_ROW_MIN || a.d > NORM_ROW_MAX) {
+        MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward<DT><<<(unsigned)a.rows, NORM_WG, 0, st>>>(a)));
+        return MLMC_OK;
+    }
+    switch (row_threads(a.d)) {
+        case 64: return forward_rows<DT, 64, 8>(a, st);
+        case 128: return forward_rows<DT, 128, 8>(a, st);
+        case 256: return forward_rows<DT, 256, 8>(a, st);
+        case 512: return forward_rows<DT, 512, 8>(a, st);
+        default: return a.d <= 8192 ? forward_rows<DT, 1024, 8>(a, st) : forward_rows<DT, 1024, 16>(a, st);
+    }
+}
+template <int DT, int T, int P> static mlmc_status backward_rows(const NormArgs& a, hipStream_t st) {
+    MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward_rows<DT, T, P, 1024><<<(unsigned)a.groups, 1024, 0, st>>>(a)));
+    return MLMC_OK;
+}
+template <int DT> static mlmc_status norm_backward(const NormArgs& a, hipStream_t st) {
+    if (a.d < NORM_ROW_MIN || a.d > NORM_ROW_MAX) {
+        const dim3 grid((unsigned)((a.d + NORM_WG - 1) / NORM_WG), (unsigned)a.groups);
+        if (a.part) MLMC_LAUNCH(K_NORM_COLUMNS, st, (k_norm_columns<DT><<<grid, NORM_WG, 0, st>>>(a)));
+        MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward<DT><<<(unsigned)a.rows, NORM_WG, 0, st>>>(a)));
+        return MLMC_OK;
+    }
+    switch (row_threads(a.d)) {
+        case 64: return backward_rows<DT, 64, 8>(a, st);
+        case 128: return backward_rows<DT, 128, 8>(a, st);
+        case 256: return backward_rows<DT, 256, 8>(a, st);
+        case 512: return backward_rows<DT, 512, 8>(a, st);
+        default: return a.d <= 8192 ? backward_rows<DT, 1024, 8>(a, st) : backward_rows<DT, 1024, 16>(a, st);
+    }
+}
 
 }  // namespace mlmc
 
@@ -128,9 +383,7 @@ mlmc_status mlmc_layer_norm(const void* x, int64_t ldx, int64_t rows, int64_t d,
     hipStream_t st = (hipStream_t)hip_stream;
     NormArgs a = {};
     a.x = x; a.ldx = ldx; a.rows = rows; a.d = d; a.weight = weight; a.bias = bias; a.eps = eps; a.y = y; a.ldy = ldy; a.stats = stats;
-    if (dtype == MLMC_F32) MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward<MLMC_F32><<<(unsigned)rows, NORM_WG, 0, st>>>(a)));
-    else MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward<MLMC_BF16><<<(unsigned)rows, NORM_WG, 0, st>>>(a)));
-    return MLMC_OK;
+    return dtype == MLMC_F32 ? norm_forward<MLMC_F32>(a, st) : norm_forward<MLMC_BF16>(a, st);
 }
 
 mlmc_status mlmc_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t rows, int64_t d, int dtype,
@@ -145,16 +398,12 @@ mlmc_status mlmc_layer_norm_backward(const void* dy, int64_t lddy, const void* x
     NormArgs a = {};
     a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.rows = rows; a.d = d; a.weight = weight; a.stats_in = stats; a.dx = dx; a.lddx = lddx;
     a.part = (float*)ws; a.groups = norm_groups(rows, d); a.dweight = dweight; a.dbias = dbias; a.grad_dtype = grad_dtype;
-    const unsigned cols = (unsigned)((d + NORM_WG - 1) / NORM_WG);
-    if (sums && rows > 0) {
-        if (dtype == MLMC_F32) MLMC_LAUNCH(K_NORM_COLUMNS, st, (k_norm_columns<MLMC_F32><<<dim3(cols, (unsigned)a.groups), NORM_WG, 0, st>>>(a)));
-        else MLMC_LAUNCH(K_NORM_COLUMNS, st, (k_norm_columns<MLMC_BF16><<<dim3(cols, (unsigned)a.groups), NORM_WG, 0, st>>>(a)));
-    }
+    if (!sums) a.part = nullptr;
     if (rows > 0) {
-        if (dtype == MLMC_F32) MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward<MLMC_F32><<<(unsigned)rows, NORM_WG, 0, st>>>(a)));
-        else MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward<MLMC_BF16><<<(unsigned)rows, NORM_WG, 0, st>>>(a)));
+        const mlmc_status rc = dtype == MLMC_F32 ? norm_backward<MLMC_F32>(a, st) : norm_backward<MLMC_BF16>(a, st);
+        if (rc != MLMC_OK) return rc;
     }
-    if (sums) MLMC_LAUNCH(K_NORM_JOIN, st, (k_norm_join<<<cols, NORM_WG, 0, st>>>(a)));
+    if (sums) MLMC_LAUNCH(K_NORM_JOIN, st, (k_norm_join<<<dim3((unsigned)((d + 63) / 64), 2), JOIN_WAVES * 64, 0, st>>>(a)));
     return MLMC_OK;
 }
 

@@ -13,16 +13,53 @@ __device__ inline float to_f32(float v) { return v; }
 __device__ inline float to_f32(__bf16 v) { return (float)v; }
 template <int DT> __device__ inline entry_t<DT> from_f32(float v) { return (entry_t<DT>)v; }   // 16 bits: to nearest, ties to even
 
+using v4f = float __attribute__((ext_vector_type(4)));
+using v8b = __bf16 __attribute__((ext_vector_type(8)));
+using chunk_t = int __attribute__((ext_vector_type(4)));                 // 16 bytes of a row
+using chunk_u = int __attribute__((ext_vector_type(4), aligned(2)));     // the same at any entry's place
+
+// 16 bytes of row `r`, columns c .. c + 16 / size - 1, of a matrix of R rows and C columns; zero outside, once cut_chunk has been over them.  A chunk
+// that the row's end cuts is taken from the row's last 16 bytes and shifted down later: no branch and no wait between the loads.  WIDE: rows
+// have 16 bytes.
+template <int DT, bool WIDE> __device__ inline chunk_t raw_chunk(const void* p, int64_t ld, int64_t r, int64_t R, int64_t c, int64_t C) {
+    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
+    const entry_t<DT>* q = (const entry_t<DT>*)p + (r < R ? r : R - 1) * ld;
+    if (WIDE || C >= E) return *(const chunk_u*)(q + (c < C - E ? c : C - E));
+    unsigned __int128 v = 0;
+#pragma unroll 1
+    for (int e = 0; e < C; ++e) v |= (unsigned __int128)(DT == MLMC_BF16 ? ((const uint16_t*)q)[e] : ((const uint32_t*)q)[e]) << (BITS * e);
+    return __builtin_bit_cast(chunk_t, v);
+}
+template <int DT, bool WIDE> __device__ inline chunk_t cut_chunk(chunk_t w, int64_t r, int64_t R, int64_t c, int64_t C) {
+    constexpr int E = DT == MLMC_BF16 ? 8 : 4, BITS = 128 / E;
+    const int64_t first = WIDE || C >= E ? C - E : 0, over = c < first ? 0 : c - first;
+    const unsigned __int128 v = __builtin_bit_cast(unsigned __int128, w);
+    return __builtin_bit_cast(chunk_t, over >= E || r >= R ? (unsigned __int128)0 : v >> (BITS * (int)over));
+}
+
+
+template <int CTRL, int ROWS> __device__ inline float dpp(float v, float outside) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, outside), __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false));
+}
+// Sum over a wave, the same in every lane: prefixes within 16 lanes, then across the four sixteens, all lane to lane (a shuffle through LDS takes ten times as long).
 __device__ inline float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v += dpp<0x111, 0xF>(v, 0.f);   // from 1, 2, 4 and 8 lanes below
+    v += dpp<0x112, 0xF>(v, 0.f);
+    v += dpp<0x114, 0xF>(v, 0.f);
+    v += dpp<0x118, 0xF>(v, 0.f);
+    v += dpp<0x142, 0xA>(v, 0.f);   // lane 15 of the sixteen below, into sixteens 1 and 3
+    v += dpp<0x143, 0xC>(v, 0.f);   // lane 31, into sixteens 2 and 3
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 // the greatest operand that is a number
 __device__ inline float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    v = fmaxf(v, dpp<0x111, 0xF>(v, v));
+    v = fmaxf(v, dpp<0x112, 0xF>(v, v));
+    v = fmaxf(v, dpp<0x114, 0xF>(v, v));
+    v = fmaxf(v, dpp<0x118, 0xF>(v, v));
+    v = fmaxf(v, dpp<0x142, 0xA>(v, v));
+    v = fmaxf(v, dpp<0x143, 0xC>(v, v));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
 // Sum over a workgroup of WAVES waves; every thread gets it, the waves' sums added in wave order.  `part`: LDS, WAVES floats,
