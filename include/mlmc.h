@@ -358,7 +358,7 @@ mlmc_status mlmc_linear_wgrad(const void *dy, int64_t lddy, const void *x, int64
  *     loss_n = T^2 sum_k q_k (log q_k - log p_{i_k}),   dlogits_nj = scale dloss_n T (p_j - sum of the q_k with i_k = j).
  * With one entry and T = 1 this is the cross entropy with label i_1.
  *   logits: dev [rows][vocab];  t_idx, t_val: dev [rows][top], 1 <= top <= MLMC_MAX_TEACHER; entries of an index below 0 are padding (their
- *   t_val is not used).  A row without an entry, or with none above -Inf, is masked: its logits are not read, loss and gradient are 0.
+ *   t_val is not used).  A row without an entry, or with none above -Inf, is masked: its loss and gradient are 0, whatever its logits.
  *   An index >= vocab makes the row's loss NaN, its gradient 0, and sets MLMC_DEV_RANGE.  A logit of -Inf has p = 0; NaN, +Inf or nothing
  *   but -Inf among a row's logits make its loss and gradient NaN.
  *   dloss: dev [rows] fp32 or NULL (1); a row whose scale * dloss is 0 has gradient 0, whatever its logits.
