@@ -301,7 +301,7 @@ mlmc_status mlmc_message_bits(const mlmc_plan_t *plan, const int32_t *level, uin
  *     function of the inputs: sums have an order that depends on sizes, types and alignment alone.
  *   - rows may be 0: nothing but weight gradients (zeros) is written, and the matrices of rows may be NULL.
  *   - ws: dev scratch, 256-byte aligned, of ws_bytes >= what the _workspace function next to the call returns for the sizes (host; 0 also for
- *     sizes that the call refuses); NULL where that is 0.
+ *     sizes that the call refuses); NULL where that is 0.  Calls that share a workspace must be ordered on one stream.
  *   - Outputs do not overlap inputs, except where a call says that they may be the same matrix (same pointer and row distance).
  */
 
@@ -328,9 +328,10 @@ mlmc_status mlmc_layer_norm_backward(const void *dy, int64_t lddy, const void *x
  * Linear layer with its epilogue: v = x weight^T + bias, y = act(v) + residual.
  *   x: dev [rows][inputs];  weight: dev [outputs][inputs];  bias: dev [outputs] or NULL;  residual: dev [rows][outputs] or NULL;
  *   z: dev [rows][outputs] (out) or NULL: receives v, which the gradient of the activation needs;  y: dev [rows][outputs] (out; may be
- *   residual).  0 <= rows, 1 <= outputs, inputs, each at most 2^21.  The workspace is that of all three calls.
+ *   residual).  0 <= rows, 1 <= outputs, inputs, each at most 2^21.
+ * The workspace is that of this call (call = 1), of mlmc_linear_dgrad (2), of mlmc_linear_wgrad (3), or enough for any of them (0).
  */
-size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs);
+size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call);
 mlmc_status mlmc_linear(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
                         const float *bias, int act, const void *residual, int64_t ldr, void *z, int64_t ldz, void *y, int64_t ldy,
                         void *ws, size_t ws_bytes, void *hip_stream);

@@ -7,6 +7,7 @@ been built (python -m paper_2507_05508_amd.build) loading fails with an error.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -86,7 +87,7 @@ def lib():
         L.mlmc_message_bits.restype = C.c_int
         L.mlmc_message_bits.argtypes = [vp, vp, vp, vp]
         f32, sz = C.c_float, C.c_size_t
-        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64]), ("mlmc_distill_workspace", [i64, i64, i32])):
+        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64, i32]), ("mlmc_distill_workspace", [i64, i64, i32])):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = args
         for name, args in (("mlmc_layer_norm", [vp, i64, i64, i64, i32, vp, vp, f32, vp, i64, vp, vp]),
@@ -349,48 +350,65 @@ def mlmc_message_bits(plan: Plan, msg, bits: Optional[torch.Tensor] = None) -> t
 _DTYPE = {torch.float32: MLMC_F32, torch.bfloat16: MLMC_BF16}
 
 
-def _rows(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
-    """Row distance of a matrix on the current device with unit inner stride; raises for anything else."""
-    sh = t.shape
-    if len(sh) != 2 or not t.is_cuda or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype) or (shape is not None and (sh[0] != shape[0] or sh[1] != shape[1])):
-        want = "float32 or bfloat16" if dtype is None else str(dtype)
-        raise MlmcError(f"{name} must be a CUDA matrix of {want}" + ("" if shape is None else f", [{shape[0]}, {shape[1]}]"))
-    if t.get_device() != torch.cuda.current_device():
-        raise MlmcError(f"{name} is not on the current device")
-    n, d = sh
-    r, c = t.stride()
-    if (c != 1 and d > 1) or (r < d and n > 1):
+def _elsewhere(t: torch.Tensor) -> bool:
+    """Not on the current CUDA device (asked without torch.cuda's check that CUDA is initialised: a CUDA tensor has done that)."""
+    at = t.get_device()
+    return at < 0 or at != torch._C._cuda_getDevice()
+
+
+def _matrix(t: torch.Tensor, name: str, dtype=None, n: int = -1, d: int = -1) -> int:
+    """Row distance of a matrix on the current device with unit inner stride ([n, d] of dtype where given); raises for anything else."""
+    try:
+        rows, cols = t.shape
+        r, c = t.stride()
+    except ValueError:
+        raise MlmcError(f"{name} must be a matrix") from None
+    if (t.dtype is not dtype and (dtype is not None or t.dtype not in _DTYPE)) or (n >= 0 and rows != n) or (d >= 0 and cols != d):
+        raise MlmcError(f"{name} must be of " + ("float32 or bfloat16" if dtype is None else str(dtype)) + f" and have the size that the others give it (it is {rows} x {cols})")
+    if _elsewhere(t):
+        raise MlmcError(f"{name} is not on the current CUDA device")
+    if (c != 1 and cols > 1) or (r < cols and rows > 1):
         raise MlmcError(f"{name} must have unit inner stride and rows that do not overlap")
-    return r if n > 1 and r > d else d
+    return r if rows > 1 and r > cols else cols
 
 
 def _vector(t: Optional[torch.Tensor], name: str, d: int, dtype=torch.float32):
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != d or not t.is_contiguous() or not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise MlmcError(f"{name} must be a contiguous CUDA tensor of {dtype}, [{d}], on the current device")
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != d or (d > 1 and t.stride(0) != 1) or _elsewhere(t):
+        raise MlmcError(f"{name} must be a contiguous tensor of {dtype}, [{d}], on the current CUDA device")
     return t.data_ptr()
 
 
-def _scratch(ws: Optional[torch.Tensor], need: int, device):
-    """The caller's workspace, or one of this call (from torch's allocator, on the current stream)."""
-    if need == 0:
-        return None, 0
+def _table(t: torch.Tensor, name: str, n: int, d: int, dtype):
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != n or t.shape[1] != d or not t.is_contiguous() or _elsewhere(t):
+        raise MlmcError(f"{name} must be a contiguous tensor of {dtype}, [{n}, {d}], on the current CUDA device")
+    return t.data_ptr()
+
+
+def _scratch(ws: Optional[torch.Tensor], need: int, like: torch.Tensor):
+    """The caller's workspace (address, bytes, tensor), or one of this call from torch's allocator, on the current stream."""
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    elif ws.dtype != torch.uint8 or not ws.is_cuda or not ws.is_contiguous() or ws.get_device() != torch.cuda.current_device():
-        raise MlmcError("ws must be a contiguous CUDA tensor of torch.uint8 on the current device")
-    return ws, ws.numel()
+        if need == 0:
+            return None, 0, None
+        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif ws.dtype is not torch.uint8 or not ws.is_contiguous() or _elsewhere(ws):
+        raise MlmcError("ws must be a contiguous tensor of torch.uint8 on the current CUDA device")
+    return ws.data_ptr(), ws.numel(), ws
 
 
+@functools.lru_cache(maxsize=4096)
 def mlmc_layer_norm_workspace(rows: int, d: int) -> int:
     return lib().mlmc_layer_norm_workspace(rows, d)
 
 
-def mlmc_linear_workspace(rows: int, outputs: int, inputs: int) -> int:
-    return lib().mlmc_linear_workspace(rows, outputs, inputs)
+@functools.lru_cache(maxsize=4096)
+def mlmc_linear_workspace(rows: int, outputs: int, inputs: int, call: int = 0) -> int:
+    """Bytes for mlmc_linear (1), mlmc_linear_dgrad (2), mlmc_linear_wgrad (3) or any of them (0)."""
+    return lib().mlmc_linear_workspace(rows, outputs, inputs, call)
 
 
+@functools.lru_cache(maxsize=4096)
 def mlmc_distill_workspace(rows: int, vocab: int, top: int) -> int:
     return lib().mlmc_distill_workspace(rows, vocab, top)
 
@@ -398,17 +416,21 @@ def mlmc_distill_workspace(rows: int, vocab: int, top: int) -> int:
 def mlmc_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                     y: Optional[torch.Tensor] = None, with_stats: bool = False, stats: Optional[torch.Tensor] = None):
     """y, or (y, stats) if the statistics for the backward pass are asked for (with_stats, or a tensor [rows, 2] that receives them)."""
-    ldx = _rows(x, "x")
+    ldx = _matrix(x, "x")
+    dtype = x.dtype
     n, d = x.shape
     if y is None:
-        y = torch.empty((n, d), dtype=x.dtype, device=x.device)
-    if stats is None and with_stats:
+        y, ldy = x.new_empty((n, d)), d
+    else:
+        ldy = _matrix(y, "y", dtype, n, d)
+    if stats is not None:
+        _table(stats, "stats", n, 2, torch.float32)
+    elif with_stats:
         stats = torch.empty((n, 2), dtype=torch.float32, device=x.device)
-    elif stats is not None and (tuple(stats.shape) != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or not stats.is_cuda):
-        raise MlmcError(f"stats must be a contiguous float32 CUDA tensor [{n}, 2]")
-    rc = lib().mlmc_layer_norm(x.data_ptr(), ldx, n, d, _DTYPE[x.dtype], _vector(weight, "weight", d), _vector(bias, "bias", d), eps,
-                               y.data_ptr(), _rows(y, "y", x.dtype, (n, d)), _ptr(stats), _stream())
-    _check(rc, "mlmc_layer_norm")
+    rc = lib().mlmc_layer_norm(x.data_ptr(), ldx, n, d, _DTYPE[dtype], _vector(weight, "weight", d), _vector(bias, "bias", d), eps,
+                               y.data_ptr(), ldy, None if stats is None else stats.data_ptr(), _stream())
+    if rc:
+        _check(rc, "mlmc_layer_norm")
     return y if stats is None else (y, stats)
 
 
@@ -416,24 +438,25 @@ def mlmc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional
                              dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
                              dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dx; dweight and dbias ([d], fp32 or bf16 alike, for instance parts of a row of the gradient matrix) are written in place."""
-    ldx = _rows(x, "x")
+    ldx = _matrix(x, "x")
+    dtype = x.dtype
     n, d = x.shape
-    if tuple(stats.shape) != (n, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or not stats.is_cuda:
-        raise MlmcError(f"stats must be a contiguous float32 CUDA tensor [{n}, 2]")
     if dx is None:
-        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
-    g = torch.float32
-    need = 0
+        dx, lddx = x.new_empty((n, d)), d
+    else:
+        lddx = _matrix(dx, "dx", dtype, n, d)
+    g, need = torch.float32, 0
     if dweight is not None or dbias is not None:
         g = (dbias if dweight is None else dweight).dtype
         if g not in _DTYPE:
             raise MlmcError("dweight and dbias must be of float32 or bfloat16")
-        need = lib().mlmc_layer_norm_workspace(n, d)
-    ws, nbytes = _scratch(ws, need, x.device)
-    rc = lib().mlmc_layer_norm_backward(dy.data_ptr(), _rows(dy, "dy", x.dtype, (n, d)), x.data_ptr(), ldx, n, d, _DTYPE[x.dtype],
-                                        _vector(weight, "weight", d), stats.data_ptr(), dx.data_ptr(), _rows(dx, "dx", x.dtype, (n, d)),
-                                        _vector(dweight, "dweight", d, g), _vector(dbias, "dbias", d, g), _DTYPE[g], _ptr(ws), nbytes, _stream())
-    _check(rc, "mlmc_layer_norm_backward")
+        need = mlmc_layer_norm_workspace(n, d)
+    p, nbytes, ws = _scratch(ws, need, x)
+    rc = lib().mlmc_layer_norm_backward(dy.data_ptr(), _matrix(dy, "dy", dtype, n, d), x.data_ptr(), ldx, n, d, _DTYPE[dtype],
+                                        _vector(weight, "weight", d), _table(stats, "stats", n, 2, torch.float32), dx.data_ptr(), lddx,
+                                        _vector(dweight, "dweight", d, g), _vector(dbias, "dbias", d, g), _DTYPE[g], p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_layer_norm_backward")
     return dx
 
 
@@ -441,19 +464,22 @@ def mlmc_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
                 residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                 ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y = act(x weight^T + bias) + residual; z, if given, receives what act is applied to."""
-    ldx, ldw = _rows(x, "x"), _rows(weight, "weight", x.dtype)
+    ldx = _matrix(x, "x")
+    dtype = x.dtype
     n, k = x.shape
+    ldw = _matrix(weight, "weight", dtype, -1, k)
     m = weight.shape[0]
-    if weight.shape[1] != k:
-        raise MlmcError(f"weight must be [outputs, {k}]")
     if y is None:
-        y = torch.empty((n, m), dtype=x.dtype, device=x.device)
-    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), x.device)
-    rc = lib().mlmc_linear(x.data_ptr(), ldx, weight.data_ptr(), ldw, n, m, k, _DTYPE[x.dtype], _vector(bias, "bias", m), act,
-                           _ptr(residual), 0 if residual is None else _rows(residual, "residual", x.dtype, (n, m)),
-                           _ptr(z), 0 if z is None else _rows(z, "z", x.dtype, (n, m)),
-                           y.data_ptr(), _rows(y, "y", x.dtype, (n, m)), _ptr(ws), nbytes, _stream())
-    _check(rc, "mlmc_linear")
+        y, ldy = x.new_empty((n, m)), m
+    else:
+        ldy = _matrix(y, "y", dtype, n, m)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 1), x)
+    rc = lib().mlmc_linear(x.data_ptr(), ldx, weight.data_ptr(), ldw, n, m, k, _DTYPE[dtype], _vector(bias, "bias", m), act,
+                           None if residual is None else residual.data_ptr(), 0 if residual is None else _matrix(residual, "residual", dtype, n, m),
+                           None if z is None else z.data_ptr(), 0 if z is None else _matrix(z, "z", dtype, n, m),
+                           y.data_ptr(), ldy, p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_linear")
     return y
 
 
@@ -461,37 +487,41 @@ def mlmc_linear_dgrad(dy: torch.Tensor, weight: torch.Tensor, act: int = MLMC_AC
                       residual: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
                       ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dx = (dy weight) act'(z) + residual, z being what the activation in front of the layer was applied to."""
-    lddy, ldw = _rows(dy, "dy"), _rows(weight, "weight", dy.dtype)
+    lddy = _matrix(dy, "dy")
+    dtype = dy.dtype
     n, m = dy.shape
+    ldw = _matrix(weight, "weight", dtype, m)
     k = weight.shape[1]
-    if weight.shape[0] != m:
-        raise MlmcError(f"weight must be [{m}, inputs]")
     if act != MLMC_ACT_NONE and z is None:
         raise MlmcError("the gradient of an activation needs z")
     if dx is None:
-        dx = torch.empty((n, k), dtype=dy.dtype, device=dy.device)
-    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), dy.device)
-    rc = lib().mlmc_linear_dgrad(dy.data_ptr(), lddy, weight.data_ptr(), ldw, n, m, k, _DTYPE[dy.dtype], act,
-                                 _ptr(z), 0 if z is None else _rows(z, "z", dy.dtype, (n, k)),
-                                 _ptr(residual), 0 if residual is None else _rows(residual, "residual", dy.dtype, (n, k)),
-                                 dx.data_ptr(), _rows(dx, "dx", dy.dtype, (n, k)), _ptr(ws), nbytes, _stream())
-    _check(rc, "mlmc_linear_dgrad")
+        dx, lddx = dy.new_empty((n, k)), k
+    else:
+        lddx = _matrix(dx, "dx", dtype, n, k)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 2), dy)
+    rc = lib().mlmc_linear_dgrad(dy.data_ptr(), lddy, weight.data_ptr(), ldw, n, m, k, _DTYPE[dtype], act,
+                                 None if z is None else z.data_ptr(), 0 if z is None else _matrix(z, "z", dtype, n, k),
+                                 None if residual is None else residual.data_ptr(), 0 if residual is None else _matrix(residual, "residual", dtype, n, k),
+                                 dx.data_ptr(), lddx, p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_linear_dgrad")
     return dx
 
 
 def mlmc_linear_wgrad(dy: torch.Tensor, x: torch.Tensor, dweight: torch.Tensor, dbias: Optional[torch.Tensor] = None,
                       ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dweight = dy^T x and, if given, dbias = sum over rows of dy, written in place (fp32 or bf16 alike)."""
-    lddy, ldx = _rows(dy, "dy"), _rows(x, "x", dy.dtype)
+    lddy = _matrix(dy, "dy")
+    dtype = dy.dtype
     n, m = dy.shape
+    ldx = _matrix(x, "x", dtype, n)
     k = x.shape[1]
-    if x.shape[0] != n:
-        raise MlmcError(f"x must be [{n}, inputs]")
-    lddw = _rows(dweight, "dweight", None, (m, k))
-    ws, nbytes = _scratch(ws, lib().mlmc_linear_workspace(n, m, k), dy.device)
-    rc = lib().mlmc_linear_wgrad(dy.data_ptr(), lddy, x.data_ptr(), ldx, n, m, k, _DTYPE[dy.dtype], dweight.data_ptr(), lddw,
-                                 _vector(dbias, "dbias", m, dweight.dtype), _DTYPE[dweight.dtype], _ptr(ws), nbytes, _stream())
-    _check(rc, "mlmc_linear_wgrad")
+    lddw = _matrix(dweight, "dweight", None, m, k)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 3), dy)
+    rc = lib().mlmc_linear_wgrad(dy.data_ptr(), lddy, x.data_ptr(), ldx, n, m, k, _DTYPE[dtype], dweight.data_ptr(), lddw,
+                                 _vector(dbias, "dbias", m, dweight.dtype), _DTYPE[dweight.dtype], p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_linear_wgrad")
     return dweight
 
 
@@ -500,20 +530,23 @@ def mlmc_distill(logits: torch.Tensor, t_idx: torch.Tensor, t_val: torch.Tensor,
                  dlogits: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """(loss of every row, scale * dloss times its gradient in the logits); the second is None if neither `grad` nor `dlogits` asks for it.
     dlogits may be the logits themselves.  dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for an index outside the vocabulary."""
-    ldl = _rows(logits, "logits")
+    ldl = _matrix(logits, "logits")
+    dtype = logits.dtype
     n, v = logits.shape
-    if (t_idx.dtype != torch.int32 or t_val.dtype != torch.float32 or t_idx.dim() != 2 or t_idx.shape[0] != n or t_val.shape != t_idx.shape
-            or not t_idx.is_contiguous() or not t_val.is_contiguous() or not t_idx.is_cuda or not t_val.is_cuda):
-        raise MlmcError(f"t_idx and t_val must be contiguous CUDA tensors of int32 and float32, [{n}, top]")
+    if t_idx.dim() != 2:
+        raise MlmcError("t_idx must be a matrix")
     top = t_idx.shape[1]
-    if dlogits is None and grad:
-        dlogits = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+    ldd = 0
+    if dlogits is not None:
+        ldd = _matrix(dlogits, "dlogits", dtype, n, v)
+    elif grad:
+        dlogits, ldd = logits.new_empty((n, v)), v
     if loss is None:
         loss = torch.empty(n, dtype=torch.float32, device=logits.device)
-    ws, nbytes = _scratch(ws, lib().mlmc_distill_workspace(n, v, top), logits.device)
-    rc = lib().mlmc_distill(logits.data_ptr(), ldl, n, v, _DTYPE[logits.dtype], t_idx.data_ptr(), t_val.data_ptr(), top, temperature,
-                            _vector(dloss, "dloss", n), scale, _vector(loss, "loss", n), _ptr(dlogits),
-                            0 if dlogits is None else _rows(dlogits, "dlogits", logits.dtype, (n, v)),
-                            _vector(dev_status, "dev_status", 1, torch.int32), _ptr(ws), nbytes, _stream())
-    _check(rc, "mlmc_distill")
+    p, nbytes, ws = _scratch(ws, mlmc_distill_workspace(n, v, top), logits)
+    rc = lib().mlmc_distill(logits.data_ptr(), ldl, n, v, _DTYPE[dtype], _table(t_idx, "t_idx", n, top, torch.int32), _table(t_val, "t_val", n, top, torch.float32),
+                            top, temperature, _vector(dloss, "dloss", n), scale, _vector(loss, "loss", n),
+                            None if dlogits is None else dlogits.data_ptr(), ldd, _vector(dev_status, "dev_status", 1, torch.int32), p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_distill")
     return loss, dlogits

@@ -37,11 +37,12 @@ __device__ inline float power(float x, float unit) { return __builtin_amdgcn_exp
 
 constexpr int T_LIVE = 1, T_BAD = 2;
 
-// The teacher's entries of a row into LDS (index -1: padding) and, with them, the logits at their places; a thread's greatest value and what it has seen.
+// The teacher's entries of a row into LDS (index -1: padding, also up to a multiple of four) and, with them, the logits at their places; a thread's greatest value and what it has seen.
 template <int DT, int T> __device__ inline void teacher_load(const DistillArgs& a, int64_t row, int32_t* at, float* u, float* gather, const float* gathered, float& tmax, int& seen) {
     const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
     tmax = -INFINITY;
     seen = 0;
+    if (threadIdx.x < 3 && a.top + threadIdx.x < DIS_TOP) at[a.top + threadIdx.x] = -1;
     for (int k = threadIdx.x; k < a.top; k += T) {
         const int32_t i = a.t_idx[row * a.top + k];
         const float t = a.t_val[row * a.top + k];
@@ -87,7 +88,14 @@ template <int DT, int T> __device__ inline void teacher_gradient(const DistillAr
         const int32_t i = at[k];
         if (i < first || i >= last) continue;
         float qs = 0.f;
-        for (int o = 0; o < a.top; ++o) qs += at[o] == i ? q[o] : 0.f;
+        for (int o = 0; o < a.top; o += 4) {   // padded with -1 to fours
+            const int4 w = *(const int4*)(at + o);
+            const float4 v = *(const float4*)(q + o);
+            qs += w.x == i ? v.x : 0.f;
+            qs += w.y == i ? v.y : 0.f;
+            qs += w.z == i ? v.z : 0.f;
+            qs += w.w == i ? v.w : 0.f;
+        }
         ds[i] = from_f32<DT>(fmaf(power(gather[k] - m, a.unit), coef, -c * qs));
     }
 }
@@ -131,8 +139,8 @@ template <int DT> __device__ inline void store_chunk(entry_t<DT>* s, int64_t col
 // workgroups share a CU, so that one loads or stores while another computes.
 template <int DT, int T, int N> __global__ __launch_bounds__(T, N <= 8 ? 8 : 4) void k_distill_row(DistillArgs a) {
     constexpr int E = DT == MLMC_BF16 ? 8 : 4, W = T / 64;
-    __shared__ float q[DIS_TOP], gather[DIS_TOP];
-    __shared__ int32_t at[DIS_TOP];
+    __shared__ __align__(16) float q[DIS_TOP], gather[DIS_TOP];
+    __shared__ __align__(16) int32_t at[DIS_TOP];
     __shared__ float part[5][W];
     __shared__ int flags[W];
     const int64_t row = blockIdx.x;
@@ -288,8 +296,9 @@ template <int DT> __global__ __launch_bounds__(PART_T) void k_distill_stats(Dist
 
 template <int DT> __global__ __launch_bounds__(PART_T) void k_distill_finish(DistillArgs a, int64_t row0) {
     constexpr int E = DT == MLMC_BF16 ? 8 : 4, W = PART_T / 64;
-    __shared__ float q[DIS_TOP], gather[DIS_TOP], part[5][W];
-    __shared__ int32_t at[DIS_TOP];
+    __shared__ __align__(16) float q[DIS_TOP], gather[DIS_TOP];
+    __shared__ float part[5][W];
+    __shared__ __align__(16) int32_t at[DIS_TOP];
     __shared__ int flags[W];
     const int64_t row = row0 + blockIdx.y, first = (int64_t)blockIdx.x * a.part_len, last = min(a.vocab, first + a.part_len);
     const int wave = threadIdx.x >> 6;

@@ -29,7 +29,8 @@ struct LinearArgs {
     int tiles_i, tiles_j;
     int splits;            // the contraction is cut into this many parts, whose sums are joined by k_linear_join
     int split_len;         // entries of the contraction of a part, a multiple of a step's
-    float* part;           // [splits][I][J], then [splits][I] for row_sum
+    float* part;           // the workspace: [splits][I][J], then [splits][I] for row_sum
+    size_t ws_bytes;
 };
 
 // The tail of the normal distribution, Phi(-|z|) = erfc(|z| / sqrt 2) / 2, and its density's exponential e^(-z^2 / 2), which the slope of gelu needs as well.  erfc by
@@ -660,6 +661,8 @@ template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs 
     const LinearPlan p = linear_plan(g.I, g.J, g.C, DT, fast);
     g.splits = p.splits;
     g.split_len = p.split_len;
+    const size_t need = linear_part_bytes(p, g.I, g.J);
+    if (need && (!g.part || (uintptr_t)g.part % 256 || g.ws_bytes < need)) return MLMC_EINVAL;
     return fast ? linear_tile<DT, AA, BA, true>(g, p.tile, st) : linear_tile<DT, AA, BA, false>(g, p.tile, st);
 }
 
@@ -679,16 +682,18 @@ using namespace mlmc;
 
 extern "C" {
 
-size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs) {
-    if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0) return 0;
+size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call) {
+    if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0 || call < 0 || call > 3) return 0;
     const int64_t size[3][3] = {{rows, outputs, inputs}, {rows, inputs, outputs}, {outputs, inputs, rows}};
     size_t most = 0;
-    for (const auto& z : size)
+    for (int c = 0; c < 3; ++c) {
+        if ((call && call != c + 1) || (c == 0 && rows <= FEW_ROWS)) continue;
         for (int dtype : {MLMC_F32, MLMC_BF16})
             for (int fast = 0; fast < (dtype == MLMC_BF16 ? 2 : 1); ++fast) {   // 32-bit entries have the same tiles either way
-                const size_t need = linear_part_bytes(linear_plan(z[0], z[1], z[2], dtype, fast), z[0], z[1]);
+                const size_t need = linear_part_bytes(linear_plan(size[c][0], size[c][1], size[c][2], dtype, fast), size[c][0], size[c][1]);
                 most = need > most ? need : most;
             }
+    }
     return most;
 }
 
@@ -700,11 +705,9 @@ mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t 
     if (rows == 0) return MLMC_OK;
     if (!entry_ptr_ok(x, dtype) || !entry_ptr_ok(weight, dtype) || !entry_ptr_ok(y, dtype) || !f32_ptr_ok(bias)) return MLMC_EINVAL;
     if ((residual && !entry_ptr_ok(residual, dtype)) || (z && !entry_ptr_ok(z, dtype))) return MLMC_EINVAL;
-    const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
-    if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
     g.a = x; g.lda = ldx; g.b = weight; g.ldb = ldw; g.I = rows; g.J = outputs; g.C = inputs;
-    g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype; g.part = (float*)ws;
+    g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype; g.part = (float*)ws; g.ws_bytes = ws_bytes;
     if (rows <= FEW_ROWS) return dtype == MLMC_F32 ? linear_few<MLMC_F32>(g, (hipStream_t)hip_stream) : linear_few<MLMC_BF16>(g, (hipStream_t)hip_stream);
     return linear_run<true, true>(g, dtype, (hipStream_t)hip_stream);
 }
@@ -717,12 +720,10 @@ mlmc_status mlmc_linear_dgrad(const void* dy, int64_t lddy, const void* weight, 
     if (rows == 0) return MLMC_OK;
     if (!entry_ptr_ok(dy, dtype) || !entry_ptr_ok(weight, dtype) || !entry_ptr_ok(dx, dtype)) return MLMC_EINVAL;
     if ((residual && !entry_ptr_ok(residual, dtype)) || (act != MLMC_ACT_NONE && !entry_ptr_ok(z, dtype))) return MLMC_EINVAL;
-    const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
-    if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
     g.a = dy; g.lda = lddy; g.b = weight; g.ldb = ldw; g.I = rows; g.J = inputs; g.C = outputs;
     g.act = act; g.slope_z = act != MLMC_ACT_NONE ? z : nullptr; g.ld_slope = ldz; g.residual = residual; g.ldr = ldr;
-    g.out = dx; g.ldo = lddx; g.out_dtype = dtype; g.part = (float*)ws;
+    g.out = dx; g.ldo = lddx; g.out_dtype = dtype; g.part = (float*)ws; g.ws_bytes = ws_bytes;
     return linear_run<true, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
@@ -731,11 +732,9 @@ mlmc_status mlmc_linear_wgrad(const void* dy, int64_t lddy, const void* x, int64
     if (!linear_sizes_ok(rows, outputs, inputs) || !entry_dtype_ok(dtype) || !entry_dtype_ok(grad_dtype) || lddy < outputs || ldx < inputs || lddw < inputs) return MLMC_EINVAL;
     if (!entry_ptr_ok(dweight, grad_dtype) || (dbias && !entry_ptr_ok(dbias, grad_dtype))) return MLMC_EINVAL;
     if (rows > 0 && (!entry_ptr_ok(dy, dtype) || !entry_ptr_ok(x, dtype))) return MLMC_EINVAL;
-    const size_t need = mlmc_linear_workspace(rows, outputs, inputs);
-    if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     LinearArgs g = {};
     g.a = dy; g.lda = lddy; g.b = x; g.ldb = ldx; g.I = outputs; g.J = inputs; g.C = rows;
-    g.act = MLMC_ACT_NONE; g.out = dweight; g.ldo = lddw; g.out_dtype = grad_dtype; g.row_sum = dbias; g.part = (float*)ws;
+    g.act = MLMC_ACT_NONE; g.out = dweight; g.ldo = lddw; g.out_dtype = grad_dtype; g.row_sum = dbias; g.part = (float*)ws; g.ws_bytes = ws_bytes;
     return linear_run<false, false>(g, dtype, (hipStream_t)hip_stream);
 }
 
