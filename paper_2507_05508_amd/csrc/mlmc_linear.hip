@@ -213,13 +213,19 @@ template <int DT> __device__ inline float chunk_sum(chunk_t a) {
     return s;
 }
 
+// How steps come to LDS: through registers (any entry's place); by loads that go there by themselves, of 16 bytes a lane, or of 4 (fp32 of any place: four times
+// the loads, which the slower products leave the time for: 1000 x 2049 x 1537 takes 80 us, through registers 88).
+enum LinearWay { WAY_REGISTERS = 0, WAY_CHUNKS, WAY_WORDS };
+
 // One operand's way from memory to LDS: 128 bytes of the contraction (a step) for T indices, by NT threads.
-template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
+template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
+    static constexpr bool WIDE = WAY == WAY_CHUNKS;   // a row has 16 bytes
     static constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 8 * E, N = T * 8 / NT;   // N: chunks a thread moves
     const void* p;
     int64_t ld, i0, I, C;
-    using off_t = std::conditional_t<WIDE, unsigned, int64_t>;
-    off_t off[N];   // byte offsets from the tile's base
+    using off_t = std::conditional_t<WAY != WAY_REGISTERS, unsigned, int64_t>;
+    static constexpr int LOADS = WAY == WAY_WORDS ? 4 * N : N;
+    off_t off[LOADS];   // byte offsets from the tile's base
 
     using L = Lds<DT, ALONG, T>;
     __device__ static int row(int q) { return q / L::W; }
@@ -227,11 +233,11 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
     __device__ void init(const void* p_, int64_t ld_, int64_t i0_, int64_t I_, int64_t C_) {
         p = p_; ld = ld_; i0 = i0_; I = I_; C = C_;
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int q = u * NT + threadIdx.x, r = row(q), c = chunk(q) * E;
+        for (int u = 0; u < LOADS; ++u) {
+            const int at = u * NT + threadIdx.x, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? at & 3 : 0), e = WAY == WAY_WORDS ? 1 : E;
             // what lies past the matrix repeats its last entries: it reaches only results that are not stored
             if (ALONG) off[u] = (off_t)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
-            else off[u] = (off_t)((r * ld + (i0 + c < I || I < E ? c : I - E - i0)) * (16 / E));
+            else off[u] = (off_t)((r * ld + (i0 + c < I || I < e ? c : I - e - i0)) * (16 / E));
         }
     }
     // a whole step, straight into LDS; `c` its first contraction index.  From `end` on nothing is read (the buffer has no entries, zeros arrive).
@@ -242,11 +248,13 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
                                               __builtin_amdgcn_readfirstlane(c < end ? -1 : 0) /* the select is compiled into a vector one */, 0x00027000);
         const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x) & ~63;
 #pragma unroll
-        for (int u = 0; u < N; ++u)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, (int)off[u], 0, 0, 0);
+        for (int u = 0; u < LOADS; ++u) {
+            if constexpr (WAY == WAY_WORDS) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)((int*)s + u * NT + wave0), 4, (int)off[u], 0, 0, 0);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, (int)off[u], 0, 0, 0);
+        }
     }
     // any step, by way of registers, zeros outside
-    __device__ bool inside(int64_t c) const { return c + STEP <= C && (ALONG || i0 + T <= I); }
+    __device__ bool inside(int64_t c) const { return WAY != WAY_WORDS && c + STEP <= C && (ALONG || i0 + T <= I); }
     __device__ void load(chunk_t (&v)[N], int64_t c) const {
         if (inside(c)) {
             const char* base = (const char*)p + (ALONG ? i0 * ld + c : c * ld + i0) * (16 / E);
@@ -277,13 +285,13 @@ template <int DT, bool ALONG, int T, int NT, bool WIDE> struct Operand {
 };
 
 // A tile of the product.  WM x WN waves, each FM x FN matrix instructions of 32 x 32.  AA, BA: the contraction is contiguous in A, B.
-// FAST: whole steps come straight into LDS.
-template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST>
+template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY>
 __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
     constexpr int NT = WM * WN * 64, TM = WM * FM * 32, TN = WN * FN * 32;
+    constexpr bool FAST = WAY != WAY_REGISTERS;   // whole steps come straight into LDS
     __shared__ chunk_t a0[TM * 8], b0[TN * 8], a1[TM * 8], b1[TN * 8];
-    using OpA = Operand<DT, AA, TM, NT, FAST>;
-    using OpB = Operand<DT, BA, TN, NT, FAST>;
+    using OpA = Operand<DT, AA, TM, NT, WAY>;
+    using OpB = Operand<DT, BA, TN, NT, WAY>;
     constexpr int STEP = OpA::STEP;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
     // neighbouring tiles to the workgroups of one die (workgroups go round the 8 dies), eight tile rows at a time
@@ -337,7 +345,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
         for (int i = 0; i < READS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            if (FAST && (q == 3 || q == 0)) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
+            if (FAST && (q == 3 || q == 0)) __builtin_amdgcn_sched_group_barrier(0x10, WAY == WAY_WORDS ? 4 : 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -628,12 +636,12 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
 }
 static size_t linear_part_bytes(const LinearPlan& p, int64_t I, int64_t J) { return p.splits > 1 ? (size_t)p.splits * (size_t)(I * J + I) * sizeof(float) : 0; }
 
-template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
+template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
     constexpr int TM = WM * FM * 32, TN = WN * FN * 32;
     g.tiles_i = (int)((g.I + TM - 1) / TM);
     g.tiles_j = (int)((g.J + TN - 1) / TN);
     const unsigned grid = (unsigned)((int64_t)g.tiles_i * g.tiles_j * g.splits);
-    MLMC_LAUNCH(K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, FAST><<<grid, WM * WN * 64, 0, st>>>(g)));
+    MLMC_LAUNCH(K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, WAY><<<grid, WM * WN * 64, 0, st>>>(g)));
     if (g.splits > 1) {
         const unsigned groups = (unsigned)((g.I * ((g.J + 7) / 8) + g.I + 255) / 256);
         MLMC_LAUNCH(K_LINEAR_JOIN, st, (k_linear_join<DT><<<groups, 256, 0, st>>>(g)));
@@ -641,29 +649,35 @@ template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, bool FAST> s
     return MLMC_OK;
 }
 
-// Whether whole steps of an operand may come straight into LDS: 16-byte chunks that are aligned and lie inside the matrix or outside, offsets within a tile that fit 32 bits.
-static bool operand_fast(const void* p, int64_t ld, int64_t width, int esize) {
+// The way of an operand: chunks that are aligned and lie inside the matrix or outside; words; offsets within a tile have to fit 32 bits for either.
+static int operand_way(const void* p, int64_t ld, int64_t width, int esize) {
     const int E = 16 / esize;
-    return (uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0 && ld <= ((int64_t)1 << 22) / esize;
+    if (ld > ((int64_t)1 << 22) / esize) return WAY_REGISTERS;
+    if ((uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0) return WAY_CHUNKS;
+    return esize == 4 ? WAY_WORDS : WAY_REGISTERS;
 }
 
-template <int DT, bool AA, bool BA, bool FAST> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
-    if constexpr (DT == MLMC_BF16 && FAST)
-        if (tile == TILE_256) return launch_tile<DT, 2, 4, 4, 2, AA, BA, FAST>(g, st);
-    if (tile == TILE_128) return launch_tile<DT, 2, 2, 2, 2, AA, BA, FAST>(g, st);
-    if (tile == TILE_64) return launch_tile<DT, 1, 4, 2, 1, AA, BA, FAST>(g, st);
-    return launch_tile<DT, 1, 4, 1, 1, AA, BA, FAST>(g, st);
+template <int DT, bool AA, bool BA, int WAY> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
+    if constexpr (DT == MLMC_BF16 && WAY == WAY_CHUNKS)
+        if (tile == TILE_256) return launch_tile<DT, 2, 4, 4, 2, AA, BA, WAY>(g, st);
+    if (tile == TILE_128) return launch_tile<DT, 2, 2, 2, 2, AA, BA, WAY>(g, st);
+    if (tile == TILE_64) return launch_tile<DT, 1, 4, 2, 1, AA, BA, WAY>(g, st);
+    return launch_tile<DT, 1, 4, 1, 1, AA, BA, WAY>(g, st);
 }
 
 template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs g, hipStream_t st) {
     constexpr int esize = DT == MLMC_BF16 ? 2 : 4;
-    const bool fast = operand_fast(g.a, g.lda, AA ? g.C : g.I, esize) && operand_fast(g.b, g.ldb, BA ? g.C : g.J, esize);
-    const LinearPlan p = linear_plan(g.I, g.J, g.C, DT, fast);
+    const int wa = operand_way(g.a, g.lda, AA ? g.C : g.I, esize), wb = operand_way(g.b, g.ldb, BA ? g.C : g.J, esize);
+    const int way = wa == WAY_REGISTERS || wb == WAY_REGISTERS ? WAY_REGISTERS : wa == WAY_CHUNKS && wb == WAY_CHUNKS ? WAY_CHUNKS : WAY_WORDS;
+    const LinearPlan p = linear_plan(g.I, g.J, g.C, DT, way == WAY_CHUNKS);
     g.splits = p.splits;
     g.split_len = p.split_len;
     const size_t need = linear_part_bytes(p, g.I, g.J);
     if (need && (!g.part || (uintptr_t)g.part % 256 || g.ws_bytes < need)) return MLMC_EINVAL;
-    return fast ? linear_tile<DT, AA, BA, true>(g, p.tile, st) : linear_tile<DT, AA, BA, false>(g, p.tile, st);
+    if (way == WAY_CHUNKS) return linear_tile<DT, AA, BA, WAY_CHUNKS>(g, p.tile, st);
+    if constexpr (DT == MLMC_F32)
+        if (way == WAY_WORDS) return linear_tile<DT, AA, BA, WAY_WORDS>(g, p.tile, st);
+    return linear_tile<DT, AA, BA, WAY_REGISTERS>(g, p.tile, st);
 }
 
 template <bool AA, bool BA> static mlmc_status linear_run(const LinearArgs& g, int dtype, hipStream_t st) {
