@@ -361,7 +361,7 @@ mlmc_status mlmc_linear_wgrad(const void *dy, int64_t lddy, const void *x, int64
  *   logits: dev [rows][vocab];  t_idx, t_val: dev [rows][top], 1 <= top <= MLMC_MAX_TEACHER; entries of an index below 0 are padding (their
  *   t_val is not used).  A row without an entry, or with none above -Inf, is masked: its loss and gradient are 0, whatever its logits.
  *   An index >= vocab makes the row's loss NaN, its gradient 0, and sets MLMC_DEV_RANGE.  A logit of -Inf has p = 0; NaN, +Inf or nothing
- *   but -Inf among a row's logits make its loss and gradient NaN.
+ *   but -Inf among a row's logits make its loss and gradient NaN; NaN or +Inf among its t_val the loss and the gradient at the teacher's indices.
  *   dloss: dev [rows] fp32 or NULL (1); a row whose scale * dloss is 0 has gradient 0, whatever its logits.
  *   loss: dev [rows] fp32 (out);  dlogits: dev [rows][ldd] (out; may be logits) or NULL: the loss alone;  dev_status: dev [1] or NULL.
  */

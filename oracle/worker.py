@@ -78,18 +78,18 @@ def distill(logits, t_idx, t_val, temperature, dloss=None, scale=1.0):
         if any(j >= v for j, _ in entries):
             loss[i] = math.nan
             continue
-        entries = [(j, t) for j, t in entries if t != -math.inf]
-        if not entries:
+        if all(t == -math.inf for _, t in entries):
             continue
-        top = max(t for _, t in entries)
-        q = np.array([math.exp((t - top) / temperature) for _, t in entries])
-        log_q = np.array([(t - top) / temperature for _, t in entries]) - math.log(q.sum())
-        q = q / q.sum()
+        t = np.array([t for _, t in entries])
+        with np.errstate(invalid="ignore", divide="ignore"):       # a NaN or +Inf among them: every q is NaN
+            q = np.exp((t - t.max()) / temperature)
+            log_q = (t - t.max()) / temperature - np.log(q.sum())
+            q = q / q.sum()
         with np.errstate(invalid="ignore", divide="ignore"):
             u = (logits[i] - logits[i].max()) / temperature
             log_p = u - np.log(np.exp(u).sum())
         for k, (j, _) in enumerate(entries):
-            if q[k] > 0:
+            if q[k] != 0:
                 loss[i] += temperature * temperature * q[k] * (log_q[k] - log_p[j])
         w = scale * (1.0 if dloss is None else float(dloss[i]))
         if w != 0.0:

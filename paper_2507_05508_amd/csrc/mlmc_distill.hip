@@ -430,7 +430,7 @@ mlmc_status mlmc_distill(const void* logits, int64_t ldl, int64_t rows, int64_t 
                          float temperature, const float* dloss, float scale, float* loss, void* dlogits, int64_t ldd, int32_t* dev_status,
                          void* ws, size_t ws_bytes, void* hip_stream) {
     if (rows < 0 || rows >= ((int64_t)1 << 31) || vocab < 1 || vocab >= ((int64_t)1 << 31) || !entry_dtype_ok(dtype) || top < 1 || top > MLMC_MAX_TEACHER) return MLMC_EINVAL;
-    if (!(temperature > 0.0f) || temperature > 3.402823e38f || !(1.0f / temperature <= 3.402823e38f) || ldl < vocab || (dlogits && ldd < vocab)) return MLMC_EINVAL;
+    if (!(temperature > 0.0f) || temperature > 3.402823e38f || !(1.4426950408889634f / temperature <= 3.402823e38f) || ldl < vocab || (dlogits && ldd < vocab)) return MLMC_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     if (!f32_ptr_ok(dev_status)) return MLMC_EINVAL;
     if (rows > 0) {

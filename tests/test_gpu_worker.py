@@ -38,8 +38,8 @@ def vec(rng, d, mean, std):
 
 def near(name, got, want, tol):
     got = f64(got)
-    off = np.abs(got - want) - tol
-    assert not np.isnan(got).any(), name
+    off = np.where(np.isnan(want), 0.0, np.abs(got - want) - tol)
+    assert (np.isnan(got) == np.isnan(want)).all(), name
     assert (off <= 0).all(), f"{name}: {off.max()} over a bound of {np.broadcast_to(tol, off.shape).reshape(-1)[off.argmax()]}"
 
 
@@ -568,3 +568,115 @@ def test_step_in_a_graph_and_on_another_stream(dtype):
 def test_the_librarys_own_kernels_run():
     names = launched(lambda: step(*head()))
     assert names and all(n.startswith(("k_norm", "k_linear", "k_distill")) for n in names), names
+
+
+# ---- sizes that take the other ways -----------------------------------------------------------------------------------
+def test_linear_large_tiles():
+    """Products large enough for the largest tile, the contraction ending inside a step; the definition on the GPU in 64 bits."""
+    n, m, k = 4072, 4088, 4040
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    make = lambda r, c, std: torch.empty((r, c), device="cuda").normal_(0.0, std, generator=gen).to(torch.bfloat16)  # noqa: E731
+    x, w, dy, z, res = make(n, k, 1.0), make(m, k, k ** -0.5), make(n, m, 0.1), make(n, k, 1.0), make(n, m, 1.0)
+    b = torch.empty(m, device="cuda").normal_(0.0, 0.3, generator=gen)
+
+    def check(name, got, want, tol):
+        off = (got.double() - want).abs() - tol
+        assert bool((off <= 0).all()), f"{name}: {float(off.max())}"
+
+    X, W, D, Z, R = (t.double() for t in (x, w, dy, z, res))
+    v = X @ W.t().contiguous() + b.double()
+    tol_v = (k + 2) * U * (X.abs() @ W.abs().t().contiguous() + b.double().abs())
+    zo = torch.empty((n, m), dtype=torch.bfloat16, device="cuda")
+    y = P.mlmc_linear(x, w, b, act=ACT["gelu"], residual=res, z=zo)
+    want = 0.5 * v * torch.erfc(-v / 2 ** 0.5) + R
+    tol = 1.13 * tol_v + (8 * U + 1e-7) * v.abs() + 2 * U * (want.abs() + R.abs())
+    check("y", y, want, tol + UO["bf16"] * (want.abs() + tol))
+    check("z", zo, v, tol_v + UO["bf16"] * (v.abs() + tol_v))
+    dx = P.mlmc_linear_dgrad(dy, w, act=ACT["gelu"], z=z)
+    v = D @ W
+    want = v * (0.5 * torch.erfc(-Z / 2 ** 0.5) + Z * torch.exp(-0.5 * Z * Z) * (2 * np.pi) ** -0.5)
+    tol = 1.13 * (m + 2) * U * (D.abs() @ W.abs()) + 2e-6 * v.abs() + 2 * U * want.abs()
+    check("dx", dx, want, tol + UO["bf16"] * (want.abs() + tol))
+    dw, db = torch.empty((m, k), device="cuda"), torch.empty(m, device="cuda")
+    P.mlmc_linear_wgrad(dy, x, dw, db)
+    check("dweight", dw, D.t().contiguous() @ X, (n + 9) * U * (D.abs().t().contiguous() @ X.abs()))
+    check("dbias", db, D.sum(0), (n + 9) * U * D.abs().sum(0))
+
+
+def test_offsets_past_32_bits():
+    """Rows two to the 28 entries apart: the last of 20 begins 10 GB behind the first."""
+    n, d, far = 20, 200, (1 << 28) + 3
+    rng = np.random.default_rng(4)
+    big = torch.empty(far * (n - 1) + d, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(big, (n, d), (far, 1), 0)
+    near_, x64 = rows(rng, n, d, "bf16")
+    x.copy_(near_)
+    w, w64 = vec(rng, d, 1.0, 0.2)
+    y, stats = P.mlmc_layer_norm(x, w, with_stats=True)
+    assert torch.equal(y, P.mlmc_layer_norm(near_, w))
+    dy, dy64 = rows(rng, n, d, "bf16")
+    dw, db = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    dx = P.mlmc_layer_norm_backward(dy, x, w, stats, dw, db)
+    dw2 = torch.empty_like(dw)
+    assert torch.equal(dx, P.mlmc_layer_norm_backward(dy, near_, w, stats, dw2)) and torch.equal(dw, dw2)
+    wt, wt64 = rows(rng, 72, d, "bf16", std=0.1)
+    for k in (3, n):                                               # the way of few rows and the tiles
+        out = torch.as_strided(big, (k, 72), (far, 1), d - 72)
+        keep = out.clone()
+        want = x64[:k] @ wt64.T
+        tol = (d + 2) * U * (np.abs(x64[:k]) @ np.abs(wt64).T)
+        got = P.mlmc_linear(x[:k], wt)
+        near("y", got, want, tol + UO["bf16"] * (np.abs(want) + tol))
+        other = torch.as_strided(torch.empty(far * (k - 1) + 72, dtype=torch.bfloat16, device="cuda"), (k, 72), (far, 1), 0)
+        P.mlmc_linear(x[:k], wt, y=other)
+        assert torch.equal(other, got) and torch.equal(out, keep)
+        del other
+    g = torch.empty((72, d), device="cuda")
+    dz, dz64 = rows(rng, n, 72, "bf16")
+    P.mlmc_linear_wgrad(dz, x, g)
+    near("dweight", g, dz64.T @ x64, (n + 8) * U * (np.abs(dz64).T @ np.abs(x64)))
+    idx, val = teacher(rng, n, d, 5, pads=False)
+    ti, tv = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(val).cuda()
+    loss, ds = P.mlmc_distill(near_, ti, tv)
+    loss2, _ = P.mlmc_distill(x, ti, tv, dlogits=x)
+    assert torch.equal(loss, loss2) and torch.equal(ds, x)
+
+
+@pytest.mark.parametrize("dtype,n", [("f32", 130), ("bf16", 250)])
+def test_distill_long_rows_in_groups(dtype, n):
+    """Rows too long for a workgroup, and more of them than one launch takes: the ends of the groups against the definition."""
+    v = 270_001
+    rng = np.random.default_rng(6)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    s = torch.empty((n, v), device="cuda").normal_(0.0, 2.0, generator=gen).to(DT[dtype])
+    idx, val = teacher(rng, n, v, 6)
+    ti, tv = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(val).cuda()
+    loss, ds = P.mlmc_distill(s, ti, tv, 2.0, scale=0.25)
+    for i in (0, 1, 2, 3, 92, 93, 94, n - 65, n - 64, n - 1):
+        want, grad, tol_loss, tol = distill_bounds(f64(s[i:i + 1]), idx[i:i + 1], val[i:i + 1].astype(np.float64), 2.0, None, 0.25)
+        near(f"loss {i}", loss[i:i + 1], want, tol_loss)
+        near(f"dlogits {i}", ds[i:i + 1], grad, tol + UO[dtype] * (np.abs(grad) + tol))
+    P.mlmc_distill(s, ti, tv, 2.0, scale=0.25, dlogits=s)
+    bits = torch.int32 if dtype == "f32" else torch.int16          # (one row's teacher has a NaN)
+    assert torch.equal(s.view(bits), ds.view(bits))
+
+
+@pytest.mark.parametrize("n,v", SHAPES)
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+def test_distill_nan_and_inf_among_the_teachers_values(n, v, what):
+    """The row's loss and its gradient at the teacher's indices are NaN, all else is as without."""
+    print(f"distill teacher {what} n={n} v={v}", flush=True)
+    rng = np.random.default_rng(8)
+    s, s64 = rows(rng, n, v)
+    idx = np.tile(np.array([3, 60, 90]), (n, 1))
+    val = rng.normal(0, 1, (n, 3)).astype(np.float32)
+    val[n - 1, 1] = what
+    loss, ds = P.mlmc_distill(s, torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(val).cuda())
+    for i in {0, n - 1}:
+        want, grad = O.distill(s64[i:i + 1], idx[i:i + 1], val[i:i + 1].astype(np.float64), 1.0)
+        assert np.isnan(want[0]) == (i == n - 1) and np.isnan(grad).sum() == (3 if i == n - 1 else 0)
+        p = np.exp(s64[i] - s64[i].max())
+        near(f"dlogits {i}", ds[i:i + 1], grad, (p / p.sum() + 1)[None] * U * (v / 64 + 200))
+    assert int(torch.isnan(loss).sum()) == 1 and bool(torch.isnan(loss[n - 1]))
