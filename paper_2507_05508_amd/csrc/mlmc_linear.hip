@@ -213,8 +213,9 @@ template <int DT> __device__ inline float chunk_sum(chunk_t a) {
     return s;
 }
 
-// How steps come to LDS: through registers (any entry's place); by loads that go there by themselves, of 16 bytes a lane, or of 4 (fp32 of any place: four times
-// the loads, which the slower products leave the time for: 1000 x 2049 x 1537 takes 80 us, through registers 88).
+// How steps come to LDS: through registers (any entry's place); by loads that go there by themselves, of 16 bytes a lane, or of 4 (fp32 of any place, bf16 whose rows
+// begin and end at 4 bytes: four times the loads).  Through registers / by words, us: fp32 1000 x 2049 x 1537 88 / 80; bf16 1000 x 2050 x 1538 forward 27.5 / 23.1,
+// input gradient 43.5 / 25.9, weight gradient 30.5 / 21.7; 4098 x 4098 over 4096 298 / 200.
 enum LinearWay { WAY_REGISTERS = 0, WAY_CHUNKS, WAY_WORDS };
 
 // One operand's way from memory to LDS: 128 bytes of the contraction (a step) for T indices, by NT threads.
@@ -234,7 +235,7 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
         p = p_; ld = ld_; i0 = i0_; I = I_; C = C_;
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int at = u * NT + threadIdx.x, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? at & 3 : 0), e = WAY == WAY_WORDS ? 1 : E;
+            const int at = u * NT + threadIdx.x, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? (at & 3) * (E / 4) : 0), e = WAY == WAY_WORDS ? E / 4 : E;
             // what lies past the matrix repeats its last entries: it reaches only results that are not stored
             if (ALONG) off[u] = (off_t)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
             else off[u] = (off_t)((r * ld + (i0 + c < I || I < e ? c : I - e - i0)) * (16 / E));
@@ -654,7 +655,7 @@ static int operand_way(const void* p, int64_t ld, int64_t width, int esize) {
     const int E = 16 / esize;
     if (ld > ((int64_t)1 << 22) / esize) return WAY_REGISTERS;
     if ((uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0) return WAY_CHUNKS;
-    return esize == 4 ? WAY_WORDS : WAY_REGISTERS;
+    return (uintptr_t)p % 4 == 0 && ld % (E / 4) == 0 && width % (E / 4) == 0 ? WAY_WORDS : WAY_REGISTERS;
 }
 
 template <int DT, bool AA, bool BA, int WAY> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
@@ -675,8 +676,7 @@ template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs 
     const size_t need = linear_part_bytes(p, g.I, g.J);
     if (need && (!g.part || (uintptr_t)g.part % 256 || g.ws_bytes < need)) return MLMC_EINVAL;
     if (way == WAY_CHUNKS) return linear_tile<DT, AA, BA, WAY_CHUNKS>(g, p.tile, st);
-    if constexpr (DT == MLMC_F32)
-        if (way == WAY_WORDS) return linear_tile<DT, AA, BA, WAY_WORDS>(g, p.tile, st);
+    if (way == WAY_WORDS) return linear_tile<DT, AA, BA, WAY_WORDS>(g, p.tile, st);
     return linear_tile<DT, AA, BA, WAY_REGISTERS>(g, p.tile, st);
 }
 

@@ -680,3 +680,11 @@ def test_distill_nan_and_inf_among_the_teachers_values(n, v, what):
         p = np.exp(s64[i] - s64[i].max())
         near(f"dlogits {i}", ds[i:i + 1], grad, (p / p.sum() + 1)[None] * U * (v / 64 + 200))
     assert int(torch.isnan(loss).sum()) == 1 and bool(torch.isnan(loss[n - 1]))
+
+
+@pytest.mark.parametrize("n,m,k,pad,shift", [(130, 70, 130, 2, 2), (70, 258, 194, 0, 0), (33, 6, 2, 0, 6), (300, 130, 4, 2, 2), (2, 2, 1000, 0, 2), (515, 262, 134, 4, 4)])
+def test_linear_of_rows_that_begin_at_four_bytes(n, m, k, pad, shift):
+    for dtype in ("bf16", "f32"):
+        test_linear(n, m, k, pad, shift, dtype)
+        test_linear_dgrad(n, m, k, pad, shift, dtype)
+        test_linear_wgrad(n, m, k, pad, shift, dtype, "bf16")
