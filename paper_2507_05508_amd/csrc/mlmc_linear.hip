@@ -4,6 +4,11 @@
 //   forward:  z = x W^T + b, y = act(z) + r         x [n][k], W [m][k]; contraction over k
 //   dgrad:    dx = (dy W) act'(z) + r               dy [n][m];          contraction over m
 //   wgrad:    dW = dy^T x, db = sum over rows of dy;                    contraction over n
+//
+// Products of many rows are bound by the matrix units and what feeds them, those of few rows by reading the weight.  Kernel times: 8192 x 4096 x 4096 bf16 with gelu,
+// v stored too, 250 us (1.1 PFLOP/s; the matrix units are busy in 55 % of the cycles at the 1.86 GHz that the card runs then; a library product without the epilogue
+// takes 177 to 220 us); input gradient 4001 x 4096 x 4096 with gelu 130 us (1.03 PFLOP/s); weight gradient 4096 x 1024 over 8192 rows, fp32 out, 73 + 10 us (the second is the
+// join of two parts; library 82 to 88); fp32 1000 x 2049 x 1537 80 us (library 78), 2048 x 2048 x 2048 124 us (139 TFLOP/s); one row of 4096 x 4096 8.6 us (3.9 TB/s).
 #include <type_traits>
 
 #include "mlmc_worker.h"
@@ -286,6 +291,10 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
 };
 
 // A tile of the product.  WM x WN waves, each FM x FN matrix instructions of 32 x 32.  AA, BA: the contraction is contiguous in A, B.
+// The large tile (256 x 256, bf16) has 8 waves of 128 x 64: two a SIMD, so that one multiplies while the other waits to issue loads or is in the epilogue.  Four waves of
+// 128 x 128 read a third less from LDS and are no faster (gelu, z stored: 8192 x 4096 x 4096 240 and 240 us, 8192 x 4096 x 1024 102 and 92; weight gradient of the former 251
+// and 228).  Four steps of 64 bytes in flight instead of two of 128 have twice the barriers, and the loads are not what is waited for (247 and 236 us for
+// 8192 x 4096 x 4096).  With no loads that product would take two thirds of the time, with nothing but loads also: what is left is that the two do not overlap fully.
 template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY>
 __global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
     constexpr int NT = WM * WN * 64, TM = WM * FM * 32, TN = WN * FN * 32;
@@ -535,7 +544,8 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArg
 }
 
 // The forward product of up to 16 rows: bound by reading the weight once.  A workgroup has 16 outputs, its waves share the contraction and each has many
-// 16-byte loads in flight, straight into the registers of the matrix instructions (16 x 16): no LDS, no second launch.  One row of 4096 x 4096 bf16: 33.6 MB.
+// 16-byte loads in flight, straight into the registers of the matrix instructions (16 x 16): no LDS, no second launch.  One row of 4096 x 4096 bf16, 33.6 MB: 8.6 us
+// (by the smallest tile in 8 parts, with its join, 13).
 constexpr int FEW_ROWS = 16, FEW_WAVES = 8, FEW_DEPTH = 8;
 template <int DT, bool WIDE> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs g) {
     constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 4 * E;   // entries of the contraction a load of a wave covers, 64 bytes of each of 16 rows
