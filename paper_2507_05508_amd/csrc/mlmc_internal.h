@@ -298,7 +298,7 @@ enum KernelId {
     K_RS_HIST, K_RS_SCAN, K_RS_SCATTER, K_SB_NORMS, K_SB_DRAW, K_SB_MARK, K_SB_OFFSETS, K_SB_WRITE, K_SE_COUNT, K_SE_SCAN, K_SE_SPLIT, K_SE_ZONE,
     K_ROW_SELECT, K_ROW_WRITE, K_C16_HIST, K_C16_REDUCE, K_C16_SCAN, K_C16_MARK, K_C16_OFFSETS, K_C16_WRITE,
     K_BITS_WORDS, K_AGG_WORDS, K_SCAN_MARKS,
-    K_NORM_FORWARD, K_NORM_BACKWARD, K_NORM_COLUMNS, K_NORM_JOIN, K_LINEAR, K_LINEAR_FEW, K_LINEAR_JOIN, K_DISTILL, K_DISTILL_STATS, K_NUM
+    K_NORM_FORWARD, K_NORM_BACKWARD, K_NORM_COLUMNS, K_NORM_JOIN, K_LINEAR, K_LINEAR_FEW, K_LINEAR_JOIN, K_LINEAR_PACK, K_DISTILL, K_DISTILL_STATS, K_NUM
 };
 extern bool g_prof_on;
 void prof_begin(int id, hipStream_t st);

@@ -43,14 +43,14 @@ struct LinearArgs {
 __device__ inline float normal_tail(float z, float& e) {
     e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
-    const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
-    return 0.5f * p * t * e;
+    const float p = fmaf(fmaf(fmaf(fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f), t, 0.5f * 1.421413741f), t, 0.5f * -0.284496736f), t, 0.5f * 0.254829592f);
+    return p * (t * e);
 }
 __device__ inline float relu(float z) { return z > 0.f || z != z ? z : 0.f; }   // a NaN stays one
 __device__ inline float gelu(float z) {
     float e;
     const float tail = normal_tail(z, e);
-    return z * (z > 0.f ? 1.0f - tail : tail);
+    return fmaf(-fminf(fabsf(z), 64.f), tail, fmaxf(z, 0.f));   // z Phi(z); the tail is 0 from 14 on, and infinity times it would be NaN
 }
 __device__ inline float gelu_slope(float z) {
     float e;
@@ -243,7 +243,7 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
             const int at = u * NT + threadIdx.x, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? (at & 3) * (E / 4) : 0), e = WAY == WAY_WORDS ? E / 4 : E;
             // what lies past the matrix repeats its last entries: it reaches only results that are not stored
             if (ALONG) off[u] = (off_t)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
-            else off[u] = (off_t)((r * ld + (i0 + c < I || I < e ? c : I - e - i0)) * (16 / E));
+            else off[u] = (off_t)((r * ld + (i0 + c < I ? c : (I - 1) / e * e - i0)) * (16 / E));
         }
     }
     // a whole step, straight into LDS; `c` its first contraction index.  From `end` on nothing is read (the buffer has no entries, zeros arrive).
@@ -619,14 +619,14 @@ constexpr TileCost tile_costs[TILES] = {{32, 128, {0.55f, 0.42f}, {0.53f, 0.28f}
 constexpr float LAUNCH_US = 5.f, JOIN_US = 3.f, JOIN_ENTRY_US = 1.6e-6f;
 constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
 
-struct LinearPlan { int tile, splits, split_len; };
+struct LinearPlan { int tile, splits, split_len; float us; };
 
 // The tile and the number of parts of the contraction that the costs above say to be the fastest: tiles come in rounds of one for every CU, a part more
 // makes the rounds finer and the join longer.
 static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool fast) {
     const int step = dtype == MLMC_BF16 ? 64 : 32;
     const int64_t steps = (C + step - 1) / step;
-    LinearPlan best = {TILE_128, 1, (int)C};
+    LinearPlan best = {TILE_128, 1, (int)C, 0.f};
     float least = 3.0e38f;
     for (int t = 0; t < TILES; ++t) {
         if (t == TILE_256 && (dtype != MLMC_BF16 || !fast)) continue;
@@ -639,7 +639,7 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
                              (s > 1 ? JOIN_US + JOIN_ENTRY_US * (float)(s * I) * (float)J : 0.f);
             if (us < least) {
                 least = us;
-                best = {t, s, (int)(len * step)};
+                best = {t, s, (int)(len * step), us};
             }
         }
     }
@@ -660,12 +660,41 @@ template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY> sta
     return MLMC_OK;
 }
 
-// The way of an operand: chunks that are aligned and lie inside the matrix or outside; words; offsets within a tile have to fit 32 bits for either.
-static int operand_way(const void* p, int64_t ld, int64_t width, int esize) {
+// The way of an operand: aligned chunks or words, which across the contraction have to lie inside the matrix or outside (along it, whole steps do); offsets within a tile have to
+// fit 32 bits for either.
+static int operand_way(const void* p, int64_t ld, int64_t width, bool along, int esize) {
     const int E = 16 / esize;
     if (ld > ((int64_t)1 << 22) / esize) return WAY_REGISTERS;
-    if ((uintptr_t)p % 16 == 0 && ld % E == 0 && width % E == 0) return WAY_CHUNKS;
-    return (uintptr_t)p % 4 == 0 && ld % (E / 4) == 0 && width % (E / 4) == 0 ? WAY_WORDS : WAY_REGISTERS;
+    if ((uintptr_t)p % 16 == 0 && ld % E == 0 && width >= E && (along || width % E == 0)) return WAY_CHUNKS;
+    return (uintptr_t)p % 4 == 0 && ld % (E / 4) == 0 && (along || width % (E / 4) == 0) ? WAY_WORDS : WAY_REGISTERS;
+}
+
+// bf16 matrices whose rows are no multiple of 16 bytes are copied to ones that are (zeros behind the rows) where the copy costs less than the slower ways: measured, those take
+// `slower` times what the tiles' costs say.  Forward, input gradient, weight gradient, us, through registers / by a copy and chunks: 4096 x 4095 x 4097 218 / 152, 304 / 201, 322 / 198;
+// 1001 x 1999 x 1535 23 / 20, 48 / 32, 32 / 26; 12175 x 1037 x 613 50 / 48, 50 / 44, 73 / 52.
+struct PackPlan { bool pack; LinearPlan plan; size_t bytes[2]; };
+static size_t packed_bytes(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)((cols + 7) / 8) * 16; }
+static PackPlan pack_plan(int64_t I, int64_t J, int64_t C, bool aa, bool ba, int way, bool pack_a, bool pack_b) {
+    PackPlan r = {false, linear_plan(I, J, C, MLMC_BF16, false), {0, 0}};
+    const int64_t a_cols = aa ? C : I, a_rows = aa ? I : C, b_cols = ba ? C : J, b_rows = ba ? J : C;
+    if ((a_cols % 8 == 0 && b_cols % 8 == 0) || a_cols < 8 || b_cols < 8 || a_rows * ((a_cols + 7) / 8) >= ((int64_t)1 << 30) || b_rows * ((b_cols + 7) / 8) >= ((int64_t)1 << 30)) return r;
+    const LinearPlan fast = linear_plan(I, J, C, MLMC_BF16, true);
+    const size_t a = pack_a ? packed_bytes(a_rows, a_cols) : 0, b = pack_b ? packed_bytes(b_rows, b_cols) : 0;
+    const float slower = way == WAY_WORDS || (aa && ba) ? 1.5f : 2.1f, copy_us = LAUNCH_US + 2.0f * (float)(a + b) / 3.0e6f;
+    if (fast.us + copy_us >= slower * r.plan.us) return r;
+    r = {true, fast, {a, b}};
+    return r;
+}
+static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+struct PackArgs { const void* from[2]; int64_t ld[2], rows[2], cols[2]; chunk_t* to[2]; unsigned groups_a; };
+__global__ __launch_bounds__(256) void k_linear_pack(PackArgs p) {
+    const int which = blockIdx.x >= p.groups_a;
+    const unsigned per_row = (unsigned)((p.cols[which] + 7) / 8), t = (blockIdx.x - (which ? p.groups_a : 0)) * 256 + threadIdx.x;
+    const unsigned r = t / per_row, c = t - r * per_row;
+    if (r >= p.rows[which]) return;
+    const chunk_t v = raw_chunk<MLMC_BF16, true>(p.from[which], p.ld[which], r, p.rows[which], (int64_t)c * 8, p.cols[which]);
+    p.to[which][t] = cut_chunk<MLMC_BF16, true>(v, r, p.rows[which], (int64_t)c * 8, p.cols[which]);
 }
 
 template <int DT, bool AA, bool BA, int WAY> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
@@ -678,13 +707,32 @@ template <int DT, bool AA, bool BA, int WAY> static mlmc_status linear_tile(Line
 
 template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs g, hipStream_t st) {
     constexpr int esize = DT == MLMC_BF16 ? 2 : 4;
-    const int wa = operand_way(g.a, g.lda, AA ? g.C : g.I, esize), wb = operand_way(g.b, g.ldb, BA ? g.C : g.J, esize);
-    const int way = wa == WAY_REGISTERS || wb == WAY_REGISTERS ? WAY_REGISTERS : wa == WAY_CHUNKS && wb == WAY_CHUNKS ? WAY_CHUNKS : WAY_WORDS;
-    const LinearPlan p = linear_plan(g.I, g.J, g.C, DT, way == WAY_CHUNKS);
+    const int wa = operand_way(g.a, g.lda, AA ? g.C : g.I, AA, esize), wb = operand_way(g.b, g.ldb, BA ? g.C : g.J, BA, esize);
+    int way = wa == WAY_REGISTERS || wb == WAY_REGISTERS ? WAY_REGISTERS : wa == WAY_CHUNKS && wb == WAY_CHUNKS ? WAY_CHUNKS : WAY_WORDS;
+    LinearPlan p;
+    size_t packed[2] = {0, 0};
+    if (DT == MLMC_BF16 && way != WAY_CHUNKS && g.C > 0) {
+        const PackPlan k = pack_plan(g.I, g.J, g.C, AA, BA, way, wa != WAY_CHUNKS, wb != WAY_CHUNKS);
+        p = k.plan;
+        if (k.pack) {
+            way = WAY_CHUNKS;
+            packed[0] = k.bytes[0];
+            packed[1] = k.bytes[1];
+        }
+    } else p = linear_plan(g.I, g.J, g.C, DT, way == WAY_CHUNKS);
     g.splits = p.splits;
     g.split_len = p.split_len;
-    const size_t need = linear_part_bytes(p, g.I, g.J);
+    const size_t parts = align256(linear_part_bytes(p, g.I, g.J)), need = parts + align256(packed[0]) + packed[1];
     if (need && (!g.part || (uintptr_t)g.part % 256 || g.ws_bytes < need)) return MLMC_EINVAL;
+    if (packed[0] || packed[1]) {
+        char* to = (char*)g.part + parts;
+        PackArgs k = {{g.a, g.b}, {g.lda, g.ldb}, {AA ? g.I : g.C, BA ? g.J : g.C}, {AA ? g.C : g.I, BA ? g.C : g.J}, {(chunk_t*)to, (chunk_t*)(to + align256(packed[0]))}, 0};
+        const unsigned groups_b = (unsigned)((packed[1] / 16 + 255) / 256);
+        k.groups_a = (unsigned)((packed[0] / 16 + 255) / 256);
+        MLMC_LAUNCH(K_LINEAR_PACK, st, (k_linear_pack<<<k.groups_a + groups_b, 256, 0, st>>>(k)));
+        if (packed[0]) { g.a = k.to[0]; g.lda = (k.cols[0] + 7) / 8 * 8; }
+        if (packed[1]) { g.b = k.to[1]; g.ldb = (k.cols[1] + 7) / 8 * 8; }
+    }
     if (way == WAY_CHUNKS) return linear_tile<DT, AA, BA, WAY_CHUNKS>(g, p.tile, st);
     if (way == WAY_WORDS) return linear_tile<DT, AA, BA, WAY_WORDS>(g, p.tile, st);
     return linear_tile<DT, AA, BA, WAY_REGISTERS>(g, p.tile, st);
@@ -714,7 +762,13 @@ size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int 
         if ((call && call != c + 1) || (c == 0 && rows <= FEW_ROWS)) continue;
         for (int dtype : {MLMC_F32, MLMC_BF16})
             for (int fast = 0; fast < (dtype == MLMC_BF16 ? 2 : 1); ++fast) {   // 32-bit entries have the same tiles either way
-                const size_t need = linear_part_bytes(linear_plan(size[c][0], size[c][1], size[c][2], dtype, fast), size[c][0], size[c][1]);
+                const size_t need = align256(linear_part_bytes(linear_plan(size[c][0], size[c][1], size[c][2], dtype, fast), size[c][0], size[c][1]));
+                most = need > most ? need : most;
+            }
+        for (int way : {WAY_WORDS, WAY_REGISTERS})
+            for (int which = 1; which < 4; ++which) {
+                const PackPlan k = pack_plan(size[c][0], size[c][1], size[c][2], c < 2, c == 0, way, which & 1, which & 2);
+                const size_t need = align256(linear_part_bytes(k.plan, size[c][0], size[c][1])) + align256(k.bytes[0]) + k.bytes[1];
                 most = need > most ? need : most;
             }
     }
