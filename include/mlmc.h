@@ -329,9 +329,10 @@ mlmc_status mlmc_layer_norm_backward(const void *dy, int64_t lddy, const void *x
  *   x: dev [rows][inputs];  weight: dev [outputs][inputs];  bias: dev [outputs] or NULL;  residual: dev [rows][outputs] or NULL;
  *   z: dev [rows][outputs] (out) or NULL: receives v, which the gradient of the activation needs;  y: dev [rows][outputs] (out; may be
  *   residual).  0 <= rows, 1 <= outputs, inputs, each at most 2^21.
- * The workspace is that of this call (call = 1), of mlmc_linear_dgrad (2), of mlmc_linear_wgrad (3), or enough for any of them (0).
+ * The workspace is that of this call (call = 1), of mlmc_linear_dgrad (2), of mlmc_linear_wgrad (3), or enough for any of them (0), for matrices of dtype, or of
+ * either (-1).
  */
-size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call);
+size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call, int dtype);
 mlmc_status mlmc_linear(const void *x, int64_t ldx, const void *weight, int64_t ldw, int64_t rows, int64_t outputs, int64_t inputs, int dtype,
                         const float *bias, int act, const void *residual, int64_t ldr, void *z, int64_t ldz, void *y, int64_t ldy,
                         void *ws, size_t ws_bytes, void *hip_stream);

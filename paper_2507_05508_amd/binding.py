@@ -87,7 +87,7 @@ def lib():
         L.mlmc_message_bits.restype = C.c_int
         L.mlmc_message_bits.argtypes = [vp, vp, vp, vp]
         f32, sz = C.c_float, C.c_size_t
-        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64, i32]), ("mlmc_distill_workspace", [i64, i64, i32])):
+        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64, i32, i32]), ("mlmc_distill_workspace", [i64, i64, i32])):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = args
         for name, args in (("mlmc_layer_norm", [vp, i64, i64, i64, i32, vp, vp, f32, vp, i64, vp, vp]),
@@ -403,9 +403,9 @@ def mlmc_layer_norm_workspace(rows: int, d: int) -> int:
 
 
 @functools.lru_cache(maxsize=4096)
-def mlmc_linear_workspace(rows: int, outputs: int, inputs: int, call: int = 0) -> int:
-    """Bytes for mlmc_linear (1), mlmc_linear_dgrad (2), mlmc_linear_wgrad (3) or any of them (0)."""
-    return lib().mlmc_linear_workspace(rows, outputs, inputs, call)
+def mlmc_linear_workspace(rows: int, outputs: int, inputs: int, call: int = 0, dtype: int = -1) -> int:
+    """Bytes for mlmc_linear (1), mlmc_linear_dgrad (2), mlmc_linear_wgrad (3) or any of them (0), of matrices of dtype or of either (-1)."""
+    return lib().mlmc_linear_workspace(rows, outputs, inputs, call, dtype)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -473,7 +473,7 @@ def mlmc_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
         y, ldy = x.new_empty((n, m)), m
     else:
         ldy = _matrix(y, "y", dtype, n, m)
-    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 1), x)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 1, _DTYPE[dtype]), x)
     rc = lib().mlmc_linear(x.data_ptr(), ldx, weight.data_ptr(), ldw, n, m, k, _DTYPE[dtype], _vector(bias, "bias", m), act,
                            None if residual is None else residual.data_ptr(), 0 if residual is None else _matrix(residual, "residual", dtype, n, m),
                            None if z is None else z.data_ptr(), 0 if z is None else _matrix(z, "z", dtype, n, m),
@@ -498,7 +498,7 @@ def mlmc_linear_dgrad(dy: torch.Tensor, weight: torch.Tensor, act: int = MLMC_AC
         dx, lddx = dy.new_empty((n, k)), k
     else:
         lddx = _matrix(dx, "dx", dtype, n, k)
-    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 2), dy)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 2, _DTYPE[dtype]), dy)
     rc = lib().mlmc_linear_dgrad(dy.data_ptr(), lddy, weight.data_ptr(), ldw, n, m, k, _DTYPE[dtype], act,
                                  None if z is None else z.data_ptr(), 0 if z is None else _matrix(z, "z", dtype, n, k),
                                  None if residual is None else residual.data_ptr(), 0 if residual is None else _matrix(residual, "residual", dtype, n, k),
@@ -517,7 +517,7 @@ def mlmc_linear_wgrad(dy: torch.Tensor, x: torch.Tensor, dweight: torch.Tensor, 
     ldx = _matrix(x, "x", dtype, n)
     k = x.shape[1]
     lddw = _matrix(dweight, "dweight", None, m, k)
-    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 3), dy)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_workspace(n, m, k, 3, _DTYPE[dtype]), dy)
     rc = lib().mlmc_linear_wgrad(dy.data_ptr(), lddy, x.data_ptr(), ldx, n, m, k, _DTYPE[dtype], dweight.data_ptr(), lddw,
                                  _vector(dbias, "dbias", m, dweight.dtype), _DTYPE[dweight.dtype], p, nbytes, _stream())
     if rc:

@@ -645,6 +645,14 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
     }
     return best;
 }
+// Whether k_linear_few takes a forward product: its workgroups read 16 rows of the weight each, at 30 KB a us by itself and 5 TB/s in all, and with few outputs there are few of them
+// (time of a call, and by tiles in parts: 5 x 512 x 7104 fp32 22.8 us and 17.3, 9 x 295 x 3200 13.4 and 17.7; bf16 1 x 1024 x 4096 7.5 and 14.5, 4 x 256 x 8192 11.8 and 14.9,
+// 16 x 4096 x 4096 10.4 and 11.7, 1 x 8192 x 8192 27.2 and 24.6).
+static bool few_rows(int64_t I, int64_t J, int64_t C, int dtype) {
+    if (I > FEW_ROWS) return false;
+    const float row = (float)C * (dtype == MLMC_BF16 ? 2.f : 4.f), alone = 16.f * row / 3.0e4f, all = (float)J * row / 5.0e6f;
+    return LAUNCH_US + (alone > all ? alone : all) <= linear_plan(I, J, C, dtype, false).us + 6.f;   // small calls wait for the second launch longer than it takes
+}
 static size_t linear_part_bytes(const LinearPlan& p, int64_t I, int64_t J) { return p.splits > 1 ? (size_t)p.splits * (size_t)(I * J + I) * sizeof(float) : 0; }
 
 template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY> static mlmc_status launch_tile(LinearArgs& g, hipStream_t st) {
@@ -754,17 +762,20 @@ using namespace mlmc;
 
 extern "C" {
 
-size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call) {
-    if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0 || call < 0 || call > 3) return 0;
+size_t mlmc_linear_workspace(int64_t rows, int64_t outputs, int64_t inputs, int call, int only) {
+    if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0 || call < 0 || call > 3 || (only != -1 && !entry_dtype_ok(only))) return 0;
     const int64_t size[3][3] = {{rows, outputs, inputs}, {rows, inputs, outputs}, {outputs, inputs, rows}};
     size_t most = 0;
     for (int c = 0; c < 3; ++c) {
-        if ((call && call != c + 1) || (c == 0 && rows <= FEW_ROWS)) continue;
-        for (int dtype : {MLMC_F32, MLMC_BF16})
+        if (call && call != c + 1) continue;
+        for (int dtype : {MLMC_F32, MLMC_BF16}) {
+            if ((only != -1 && dtype != only) || (c == 0 && few_rows(rows, outputs, inputs, dtype))) continue;
             for (int fast = 0; fast < (dtype == MLMC_BF16 ? 2 : 1); ++fast) {   // 32-bit entries have the same tiles either way
                 const size_t need = align256(linear_part_bytes(linear_plan(size[c][0], size[c][1], size[c][2], dtype, fast), size[c][0], size[c][1]));
                 most = need > most ? need : most;
             }
+        }
+        if (only == MLMC_F32 || (c == 0 && few_rows(rows, outputs, inputs, MLMC_BF16))) continue;
         for (int way : {WAY_WORDS, WAY_REGISTERS})
             for (int which = 1; which < 4; ++which) {
                 const PackPlan k = pack_plan(size[c][0], size[c][1], size[c][2], c < 2, c == 0, way, which & 1, which & 2);
@@ -786,7 +797,7 @@ mlmc_status mlmc_linear(const void* x, int64_t ldx, const void* weight, int64_t 
     LinearArgs g = {};
     g.a = x; g.lda = ldx; g.b = weight; g.ldb = ldw; g.I = rows; g.J = outputs; g.C = inputs;
     g.act = act; g.bias = bias; g.residual = residual; g.ldr = ldr; g.z = z; g.ldz = ldz; g.out = y; g.ldo = ldy; g.out_dtype = dtype; g.part = (float*)ws; g.ws_bytes = ws_bytes;
-    if (rows <= FEW_ROWS) return dtype == MLMC_F32 ? linear_few<MLMC_F32>(g, (hipStream_t)hip_stream) : linear_few<MLMC_BF16>(g, (hipStream_t)hip_stream);
+    if (few_rows(rows, outputs, inputs, dtype)) return dtype == MLMC_F32 ? linear_few<MLMC_F32>(g, (hipStream_t)hip_stream) : linear_few<MLMC_BF16>(g, (hipStream_t)hip_stream);
     return linear_run<true, true>(g, dtype, (hipStream_t)hip_stream);
 }
 

@@ -688,3 +688,10 @@ def test_linear_of_rows_that_begin_at_four_bytes(n, m, k, pad, shift):
         test_linear(n, m, k, pad, shift, dtype)
         test_linear_dgrad(n, m, k, pad, shift, dtype)
         test_linear_wgrad(n, m, k, pad, shift, dtype, "bf16")
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 48, 9000), (3, 40, 20000), (16, 16, 20003)])
+def test_linear_few_rows_few_outputs_long_contraction(n, m, k):
+    for dtype in ("bf16", "f32"):
+        test_linear(n, m, k, 0, 0, dtype)
+        test_linear(n, m, k, 3, 1, dtype)
