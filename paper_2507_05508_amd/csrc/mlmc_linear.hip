@@ -544,8 +544,8 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_join(LinearArg
 }
 
 // The forward product of up to 16 rows: bound by reading the weight once.  A workgroup has 16 outputs, its waves share the contraction and each has many
-// 16-byte loads in flight, straight into the registers of the matrix instructions (16 x 16): no LDS, no second launch.  One row of 4096 x 4096 bf16, 33.6 MB: 8.6 us
-// (by the smallest tile in 8 parts, with its join, 13).
+// 16-byte loads in flight, straight into the registers of the matrix instructions (16 x 16): no LDS, no second launch.  One row of 4096 x 4096 bf16, 33.6 MB: 8.6 us,
+// a call again and again 8.1 to 10.4 (by tiles in parts, with the join, 12.6).
 constexpr int FEW_ROWS = 16, FEW_WAVES = 8, FEW_DEPTH = 8;
 template <int DT, bool WIDE> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs g) {
     constexpr int E = DT == MLMC_BF16 ? 8 : 4, STEP = 4 * E;   // entries of the contraction a load of a wave covers, 64 bytes of each of 16 rows
