@@ -182,12 +182,13 @@ template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG) void k_
     for (int64_t base = (int64_t)blockIdx.x * R; base < a.rows; base += a.groups * R, row += a.groups * R, odd ^= 1) {
         if (!AHEAD) fetch(row);
         float h[P], c[P], s = 0.f, q = 0.f;
-        const float mean = ns.x, rstd = ns.y;
+        float mean = ns.x, rstd = ns.y;
         of.to_floats(h, nx);
         of.to_floats(c, ny);
-        if (R > 1 && row >= a.rows) {   // the last round's rows that are not there
+        if (R > 1 && row >= a.rows) {   // the last round's rows that are not there: what was read is the last row, or where dx is x or dy, what another wave has put there, Inf and NaN too
+            mean = rstd = 0.f;
 #pragma unroll
-            for (int e = 0; e < P; ++e) c[e] = 0.f;
+            for (int e = 0; e < P; ++e) h[e] = c[e] = 0.f;
         }
         if (AHEAD) fetch(row + a.groups * R);
 #pragma unroll

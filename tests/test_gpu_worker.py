@@ -695,3 +695,34 @@ def test_linear_few_rows_few_outputs_long_contraction(n, m, k):
     for dtype in ("bf16", "f32"):
         test_linear(n, m, k, 0, 0, dtype)
         test_linear(n, m, k, 3, 1, dtype)
+
+
+def same(name, a, b):
+    """Equal entry by entry, NaN with NaN."""
+    assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a, nan=0.0), torch.nan_to_num(b, nan=0.0)), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 8), (17, 24), (500, 320), (4099, 512), (3, 520), (2051, 1000), (5, 1500), (1027, 2048), (3, 2056), (515, 4096), (7, 8191), (5, 16384), (3, 5), (4, 16400)])
+def test_layer_norm_backward_in_the_place_of_x(n, d, dtype):
+    """dx in the place of x, or of dy, with an Inf in the last row's gradient: its dx is not finite, and dweight and dbias are those of a call with a dx of its own, where a single
+    column is not finite."""
+    print(f"layer_norm_backward in place n={n} d={d} {dtype}", flush=True)
+    rng = np.random.default_rng(n + d)
+    x, _ = rows(rng, n, d, dtype)
+    dy, _ = rows(rng, n, d, dtype, std=0.1)
+    dy[n - 1, d // 2] = float("inf")
+    w, _ = vec(rng, d, 1.0, 0.3)
+    _, stats = P.mlmc_layer_norm(x, w, None, with_stats=True)
+    dw, db = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    dx = P.mlmc_layer_norm_backward(dy, x, w, stats, dw, db)
+    assert not bool(torch.isfinite(dx[n - 1]).any()) and bool(torch.isfinite(dx[:n - 1]).all())
+    off = (~torch.isfinite(dw)).nonzero().flatten().tolist()
+    assert off == [d // 2] and (~torch.isfinite(db)).nonzero().flatten().tolist() == [d // 2]
+    for place in ("x", "dy"):
+        x2, dy2 = x.clone(), dy.clone()
+        dw2, db2 = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+        P.mlmc_layer_norm_backward(dy2, x2, w, stats, dw2, db2, dx=x2 if place == "x" else dy2)
+        same("dx in " + place, x2 if place == "x" else dy2, dx)
+        same("dweight, dx in " + place, dw2, dw)
+        same("dbias, dx in " + place, db2, db)
