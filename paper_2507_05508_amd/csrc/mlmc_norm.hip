@@ -19,6 +19,7 @@ constexpr int NORM_WG = 256;
 struct NormArgs {
     const void *x, *dy;
     int64_t ldx, lddy, rows, d;
+    int64_t row0;         // first row of a launch of a workgroup a row
     const float *weight, *bias, *stats_in;
     float eps;
     void *y, *dx;
@@ -240,8 +241,9 @@ template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG) void k_
 // One workgroup per row, which it reads three times; the second and third read come from the caches (1000 x 20000 fp32: 100 us, 1.6 TB/s of x and y).
 template <int DT> __global__ __launch_bounds__(NORM_WG) void k_norm_forward(NormArgs a) {
     __shared__ float part[2][NORM_WG / 64];
-    const entry_t<DT>* x = (const entry_t<DT>*)a.x + (int64_t)blockIdx.x * a.ldx;
-    entry_t<DT>* y = (entry_t<DT>*)a.y + (int64_t)blockIdx.x * a.ldy;
+    const int64_t row = a.row0 + blockIdx.x;
+    const entry_t<DT>* x = (const entry_t<DT>*)a.x + row * a.ldx;
+    entry_t<DT>* y = (entry_t<DT>*)a.y + row * a.ldy;
     float s = 0.f;
     for (int64_t j = threadIdx.x; j < a.d; j += NORM_WG) s += to_f32(x[j]);
     const float mean = group_sum<NORM_WG / 64>(s, part[0]) / (float)a.d;
@@ -256,17 +258,18 @@ template <int DT> __global__ __launch_bounds__(NORM_WG) void k_norm_forward(Norm
         y[j] = from_f32<DT>(fmaf(h, a.weight ? a.weight[j] : 1.0f, a.bias ? a.bias[j] : 0.0f));
     }
     if (a.stats && threadIdx.x == 0) {
-        a.stats[2 * (int64_t)blockIdx.x] = mean;
-        a.stats[2 * (int64_t)blockIdx.x + 1] = rstd;
+        a.stats[2 * row] = mean;
+        a.stats[2 * row + 1] = rstd;
     }
 }
 
 template <int DT> __global__ __launch_bounds__(NORM_WG) void k_norm_backward(NormArgs a) {
     __shared__ float part[2][NORM_WG / 64];
-    const entry_t<DT>* x = (const entry_t<DT>*)a.x + (int64_t)blockIdx.x * a.ldx;
-    const entry_t<DT>* dy = (const entry_t<DT>*)a.dy + (int64_t)blockIdx.x * a.lddy;
-    entry_t<DT>* dx = (entry_t<DT>*)a.dx + (int64_t)blockIdx.x * a.lddx;
-    const float mean = a.stats_in[2 * (int64_t)blockIdx.x], rstd = a.stats_in[2 * (int64_t)blockIdx.x + 1];
+    const int64_t row = a.row0 + blockIdx.x;
+    const entry_t<DT>* x = (const entry_t<DT>*)a.x + row * a.ldx;
+    const entry_t<DT>* dy = (const entry_t<DT>*)a.dy + row * a.lddy;
+    entry_t<DT>* dx = (entry_t<DT>*)a.dx + row * a.lddx;
+    const float mean = a.stats_in[2 * row], rstd = a.stats_in[2 * row + 1];
     float s = 0.f, t = 0.f;
     for (int64_t j = threadIdx.x; j < a.d; j += NORM_WG) {
         const float c = to_f32(dy[j]) * (a.weight ? a.weight[j] : 1.0f);
@@ -340,9 +343,12 @@ template <int DT, int T, int P> static mlmc_status forward_rows(const NormArgs& 
     MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward_rows<DT, T, P, WG><<<(unsigned)(all < most ? all : most), WG, 0, st>>>(a)));
     return MLMC_OK;
 }
-template <int DT> static mlmc_status norm_forward(const NormArgs& a, hipStream_t st) {
+constexpr int64_t NORM_SLICE = LAUNCH_THREADS / NORM_WG;   // rows of a launch of a workgroup a row
+static unsigned slice_rows(const NormArgs& a) { return (unsigned)(a.rows - a.row0 < NORM_SLICE ? a.rows - a.row0 : NORM_SLICE); }
+
+template <int DT> static mlmc_status norm_forward(NormArgs a, hipStream_t st) {
     if (a.d < NORM_ROW_MIN || a.d > NORM_ROW_MAX) {
-        MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward<DT><<<(unsigned)a.rows, NORM_WG, 0, st>>>(a)));
+        for (; a.row0 < a.rows; a.row0 += NORM_SLICE) MLMC_LAUNCH(K_NORM_FORWARD, st, (k_norm_forward<DT><<<slice_rows(a), NORM_WG, 0, st>>>(a)));
         return MLMC_OK;
     }
     switch (row_threads(a.d)) {
@@ -357,11 +363,11 @@ template <int DT, int T, int P> static mlmc_status backward_rows(const NormArgs&
     MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward_rows<DT, T, P, 1024><<<(unsigned)a.groups, 1024, 0, st>>>(a)));
     return MLMC_OK;
 }
-template <int DT> static mlmc_status norm_backward(const NormArgs& a, hipStream_t st) {
+template <int DT> static mlmc_status norm_backward(NormArgs a, hipStream_t st) {
     if (a.d < NORM_ROW_MIN || a.d > NORM_ROW_MAX) {
         const dim3 grid((unsigned)((a.d + NORM_WG - 1) / NORM_WG), (unsigned)a.groups);
         if (a.part) MLMC_LAUNCH(K_NORM_COLUMNS, st, (k_norm_columns<DT><<<grid, NORM_WG, 0, st>>>(a)));
-        MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward<DT><<<(unsigned)a.rows, NORM_WG, 0, st>>>(a)));
+        for (; a.row0 < a.rows; a.row0 += NORM_SLICE) MLMC_LAUNCH(K_NORM_BACKWARD, st, (k_norm_backward<DT><<<slice_rows(a), NORM_WG, 0, st>>>(a)));
         return MLMC_OK;
     }
     switch (row_threads(a.d)) {

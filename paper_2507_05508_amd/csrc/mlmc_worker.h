@@ -85,6 +85,9 @@ template <int WAVES> __device__ inline float group_max(float v, float* part) {
     return s;
 }
 
+// A launch has less than 2^32 threads along an axis: of more, some workgroups never run, and no error is reported.  Kernels that may need more are launched in slices.
+constexpr int64_t LAUNCH_THREADS = (int64_t)1 << 31;
+
 inline bool entry_dtype_ok(int dtype) { return dtype == MLMC_F32 || dtype == MLMC_BF16; }
 // pointers of entries have to be aligned to an entry, no more
 inline bool entry_ptr_ok(const void* p, int dtype) { return p && (uintptr_t)p % (dtype == MLMC_BF16 ? 2 : 4) == 0; }
