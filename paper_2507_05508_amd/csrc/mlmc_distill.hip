@@ -18,6 +18,7 @@ constexpr int DIS_TOP = MLMC_MAX_TEACHER;
 struct DistillArgs {
     const void* s;
     int64_t lds, rows, vocab;
+    int64_t row0;                 // first row of a launch of a workgroup a row
     const int32_t* t_idx;
     const float* t_val;
     int top;
@@ -147,7 +148,7 @@ template <int DT, int T, int N> __global__ __launch_bounds__(T, N <= 8 ? 8 : 4) 
     __shared__ __align__(16) int32_t at[DIS_TOP];
     __shared__ float part[5][W];
     __shared__ int flags[W];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const int wave = threadIdx.x >> 6, V = (int)a.vocab, lane_col = threadIdx.x * E;
     const bool first_lane = (threadIdx.x & 63) == 0;
     const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
@@ -398,15 +399,21 @@ static DistillPlan distill_plan(int64_t rows, int64_t vocab, int dtype) {
 
 using namespace mlmc;
 
+template <int DT, int T, int N> static mlmc_status distill_rows(DistillArgs& a, hipStream_t st) {
+    constexpr int64_t slice = LAUNCH_THREADS / T;
+    for (; a.row0 < a.rows; a.row0 += slice) {
+        const unsigned rows = (unsigned)(a.rows - a.row0 < slice ? a.rows - a.row0 : slice);
+        MLMC_LAUNCH(K_DISTILL, st, (k_distill_row<DT, T, N><<<rows, T, 0, st>>>(a)));
+    }
+    return MLMC_OK;
+}
 template <int DT> static mlmc_status distill_run(DistillArgs& a, const DistillPlan& p, hipStream_t st) {
-    const unsigned rows = (unsigned)a.rows;
     constexpr int64_t E = DT == MLMC_BF16 ? 8 : 4;
     if (p.parts == 0) {
-        if (a.vocab <= 256 * 4 * E) MLMC_LAUNCH(K_DISTILL, st, (k_distill_row<DT, 256, 4><<<rows, 256, 0, st>>>(a)));
-        else if (a.vocab <= 512 * 8 * E) MLMC_LAUNCH(K_DISTILL, st, (k_distill_row<DT, 512, 8><<<rows, 512, 0, st>>>(a)));
-        else if (a.vocab <= 1024 * 8 * E) MLMC_LAUNCH(K_DISTILL, st, (k_distill_row<DT, 1024, 8><<<rows, 1024, 0, st>>>(a)));
-        else MLMC_LAUNCH(K_DISTILL, st, (k_distill_row<DT, 1024, 16><<<rows, 1024, 0, st>>>(a)));
-        return MLMC_OK;
+        if (a.vocab <= 256 * 4 * E) return distill_rows<DT, 256, 4>(a, st);
+        if (a.vocab <= 512 * 8 * E) return distill_rows<DT, 512, 8>(a, st);
+        if (a.vocab <= 1024 * 8 * E) return distill_rows<DT, 1024, 8>(a, st);
+        return distill_rows<DT, 1024, 16>(a, st);
     }
     a.part_len = ((a.vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
     a.parts = (int)((a.vocab + a.part_len - 1) / a.part_len);

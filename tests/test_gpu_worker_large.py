@@ -87,3 +87,22 @@ def test_layer_norm_of_more_rows_than_a_launch_has_workgroups():
     check("dx", dx, want, tol, U)
     check("dweight", dw, want_w, tol_w, U)
     check("dbias", db, want_b, tol_b, U)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_distill_of_more_rows_than_a_launch_has_workgroups(dtype):
+    n, v, temp = (1 << 24) + 3, 5, 2.0
+    gen = generator(2)
+    s = normal(gen, n, v, dtype, 2.0)
+    at = torch.randint(0, v, (n, 1), device="cuda", generator=gen, dtype=torch.int32)
+    loss, ds = P.mlmc_distill(s, at, torch.zeros((n, 1), device="cuda"), temp, scale=0.25)
+    # one entry a teacher: q is 1 (the bounds of test_gpu_worker.distill_bounds with that)
+    z = s.double()
+    arg = (z.max(1, keepdim=True).values - z) / temp
+    log_p = -arg - torch.exp(-arg).sum(1, keepdim=True).log()
+    p = log_p.exp()
+    rel = U * (4 * arg + 4 * (p * arg).sum(1, keepdim=True) + v / 64 + 80)
+    hot = torch.zeros_like(p).scatter_(1, at.long(), 1.0)
+    check("dlogits", ds, 0.25 * temp * (p - hot), 0.25 * temp * (p * rel + hot * U * 81 + 4 * U * (p + hot)), UO[dtype])
+    log_p, arg, rel = (t.gather(1, at.long())[:, 0] for t in (log_p, arg, rel))
+    check("loss", loss, -temp * temp * log_p, temp * temp * (arg * 6 * U + rel + 81 * U + 4 * U * log_p.abs() + (81 + 9) * U * log_p.abs()) + 4 * U * temp * temp * log_p.abs())
