@@ -27,6 +27,7 @@ struct NormArgs {
     float* stats;
     float* part;          // [groups][2][d] sums of a group's rows
     int64_t groups;
+    int64_t col0;         // first column of a launch of the join
     void *dweight, *dbias;
     int grad_dtype;
 };
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void k_norm_join(NormArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = blockIdx.y;   // 0: dweight, 1: dbias
     void* out = which ? a.dbias : a.dweight;
     if (!out) return;
-    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t j = a.col0 + (int64_t)blockIdx.x * 64 + lane;
     float v = 0.f;
     if (j < a.d) {
 #pragma unroll 8
@@ -417,7 +418,11 @@ mlmc_status mlmc_layer_norm_backward(const void* dy, int64_t lddy, const void* x
         const mlmc_status rc = dtype == MLMC_F32 ? norm_backward<MLMC_F32>(a, st) : norm_backward<MLMC_BF16>(a, st);
         if (rc != MLMC_OK) return rc;
     }
-    if (sums) MLMC_LAUNCH(K_NORM_JOIN, st, (k_norm_join<<<dim3((unsigned)((d + 63) / 64), 2), JOIN_WAVES * 64, 0, st>>>(a)));
+    constexpr int64_t slice = LAUNCH_THREADS / JOIN_WAVES;   // columns of a launch: 64 a workgroup, each by a thread of every wave
+    for (; sums && a.col0 < d; a.col0 += slice) {
+        const int64_t cols = d - a.col0 < slice ? d - a.col0 : slice;
+        MLMC_LAUNCH(K_NORM_JOIN, st, (k_norm_join<<<dim3((unsigned)((cols + 63) / 64), 2), JOIN_WAVES * 64, 0, st>>>(a)));
+    }
     return MLMC_OK;
 }
 

@@ -106,3 +106,15 @@ def test_distill_of_more_rows_than_a_launch_has_workgroups(dtype):
     check("dlogits", ds, 0.25 * temp * (p - hot), 0.25 * temp * (p * rel + hot * U * 81 + 4 * U * (p + hot)), UO[dtype])
     log_p, arg, rel = (t.gather(1, at.long())[:, 0] for t in (log_p, arg, rel))
     check("loss", loss, -temp * temp * log_p, temp * temp * (arg * 6 * U + rel + 81 * U + 4 * U * log_p.abs() + (81 + 9) * U * log_p.abs()) + 4 * U * temp * temp * log_p.abs())
+
+
+def test_layer_norm_backward_of_more_columns_than_a_launch_has_workgroups():
+    """One row: dweight and dbias have one term each, the same bits as elementary operations give."""
+    d = (1 << 28) + 65
+    gen = generator(3)
+    x, dy = normal(gen, 1, d, "bf16"), normal(gen, 1, d, "bf16", 0.1)
+    stats = torch.tensor([[0.25, 1.5]], device="cuda")
+    dw, db = torch.full((d,), 7.0, device="cuda"), torch.full((d,), 7.0, device="cuda")
+    P.mlmc_layer_norm_backward(dy, x, None, stats, dw, db)
+    assert torch.equal(db, dy[0].float())
+    assert torch.equal(dw, (x[0].float() - 0.25) * 1.5 * dy[0].float())
