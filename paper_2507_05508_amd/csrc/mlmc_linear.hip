@@ -55,7 +55,7 @@ __device__ inline float gelu(float z) {
 __device__ inline float gelu_slope(float z) {
     float e;
     const float tail = normal_tail(z, e);
-    return fmaf(z * 0.39894228040143268f, e, z > 0.f ? 1.0f - tail : tail);
+    return fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228040143268f, e, z > 0.f ? 1.0f - tail : tail);   // z within +-64 for the same reason; a NaN comes by e
 }
 __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
     if (dtype == MLMC_F32) ((float*)p)[at] = v;

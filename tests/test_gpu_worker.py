@@ -699,7 +699,7 @@ def test_linear_few_rows_few_outputs_long_contraction(n, m, k):
 
 def same(name, a, b):
     """Equal entry by entry, NaN with NaN."""
-    assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a, nan=0.0), torch.nan_to_num(b, nan=0.0)), name
+    assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.where(torch.isnan(a), 0.0, a), torch.where(torch.isnan(b), 0.0, b)), name
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -726,3 +726,25 @@ def test_layer_norm_backward_in_the_place_of_x(n, d, dtype):
         same("dx in " + place, x2 if place == "x" else dy2, dx)
         same("dweight, dx in " + place, dw2, dw)
         same("dbias, dx in " + place, db2, db)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,m", [(3, 8), (40, 8), (40, 4096)])      # a tile, and one in parts with a join
+def test_activations_at_infinity(n, m, dtype):
+    """Where the activation is a straight line already, infinity is on it: the slope of gelu and relu is 1 at +Inf and 0 at -Inf, gelu(-Inf) = 0; NaN stays NaN (the slope of relu
+    is a comparison, 0 there)."""
+    top = float(torch.finfo(DT[dtype]).max)
+    z = torch.tensor([float("inf"), -float("inf"), float("nan"), top, -top, 1e30, -1e30, 70.0, -70.0, 0.0], device="cuda").to(DT[dtype])
+    k = z.numel()
+    dy = torch.zeros((n, m), dtype=DT[dtype], device="cuda")
+    dy[:, 0] = 2.0
+    w = torch.zeros((m, k), dtype=DT[dtype], device="cuda")
+    w[0] = 1.0
+    for kind, at_zero in (("gelu", 1.0), ("relu", 0.0)):
+        dx = P.mlmc_linear_dgrad(dy, w, act=ACT[kind], z=z.expand(n, k).contiguous())
+        want = torch.tensor([2.0, 0.0, float("nan") if kind == "gelu" else 0.0, 2.0, 0.0, 2.0, 0.0, 2.0, 0.0, at_zero], device="cuda").to(DT[dtype])
+        same("dx " + kind, dx, want.expand(n, k))
+    x, one = z[:, None].contiguous(), torch.ones((1, 1), dtype=DT[dtype], device="cuda")
+    for kind in ("gelu", "relu"):
+        y = P.mlmc_linear(x, one, act=ACT[kind])[:, 0]
+        same("y " + kind, y, torch.tensor([float("inf"), 0.0, float("nan"), top, 0.0, 1e30, 0.0, 70.0, 0.0, 0.0], device="cuda").to(DT[dtype]))
