@@ -38,24 +38,32 @@ struct LinearArgs {
     size_t ws_bytes;
 };
 
-// The tail of the normal distribution, Phi(-|z|) = erfc(|z| / sqrt 2) / 2, and its density's exponential e^(-z^2 / 2), which the slope of gelu needs as well.  erfc by
-// the rational approximation 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: off by at most 1.5e-7, half of which reaches Phi.
-__device__ inline float normal_tail(float z, float& e) {
+// The tail of the normal distribution, Phi(-|z|) = erfc(|z| / sqrt 2) / 2, and its density's exponential e^(-z^2 / 2), which the slope of gelu needs as well.  For 32-bit results by
+// the library's functions, so that gelu and its slope are no further off than elementary operations (2048 x 2048 x 2048 with gelu 131 us, its input gradient 134; by the approximation
+// 127 and 128, and two to three times as far off).  For 16-bit ones by the rational approximation 7.1.26 of Abramowitz and Stegun,
+// Handbook of Mathematical Functions: off by at most 1.5e-7, half of which reaches Phi, less than such a result's rounding down to z = -4 and about as much at -5.  It takes 15 to 40 us
+// less on the largest products, which have 16 bits.
+template <int DT> __device__ inline float normal_tail(float z, float& e) {
+    if constexpr (DT == MLMC_F32) {
+        e = expf(-0.5f * z * z);
+        return 0.5f * erfcf(fabsf(z) * 0.70710678118654752f);
+    }
     e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
     const float p = fmaf(fmaf(fmaf(fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f), t, 0.5f * 1.421413741f), t, 0.5f * -0.284496736f), t, 0.5f * 0.254829592f);
     return p * (t * e);
 }
 __device__ inline float relu(float z) { return z > 0.f || z != z ? z : 0.f; }   // a NaN stays one
-__device__ inline float gelu(float z) {
+template <int DT> __device__ inline float gelu(float z) {
     float e;
-    const float tail = normal_tail(z, e);
+    const float tail = normal_tail<DT>(z, e);
     return fmaf(-fminf(fabsf(z), 64.f), tail, fmaxf(z, 0.f));   // z Phi(z); the tail is 0 from 14 on, and infinity times it would be NaN
 }
-__device__ inline float gelu_slope(float z) {
+template <int DT> __device__ inline float gelu_slope(float z) {
     float e;
-    const float tail = normal_tail(z, e);
-    return fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228040143268f, e, z > 0.f ? 1.0f - tail : tail);   // z within +-64 for the same reason; a NaN comes by e
+    const float tail = normal_tail<DT>(z, e);
+    const float s = fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228040143268f, e, z > 0.f ? -tail : tail);   // z within +-64 for the same reason; a NaN comes by e
+    return z > 0.f ? 1.0f + s : s;
 }
 __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
     if (dtype == MLMC_F32) ((float*)p)[at] = v;
@@ -123,10 +131,10 @@ struct Epilogue {
         if (g.act == MLMC_ACT_GELU) {   // the branches outside of the loops: inside they took longer than the arithmetic
             if (g.slope_z) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= gelu_slope(slope[e]);
+                for (int e = 0; e < 8; ++e) v[e] *= gelu_slope<DT>(slope[e]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = gelu(v[e]);
+                for (int e = 0; e < 8; ++e) v[e] = gelu<DT>(v[e]);
             }
         } else if (g.act == MLMC_ACT_RELU) {
             if (g.slope_z) {
@@ -295,8 +303,9 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
 // 128 x 128 read a third less from LDS and are no faster (gelu, z stored: 8192 x 4096 x 4096 240 and 240 us, 8192 x 4096 x 1024 102 and 92; weight gradient of the former 251
 // and 228).  Four steps of 64 bytes in flight instead of two of 128 have twice the barriers, and the loads are not what is waited for (247 and 236 us for
 // 8192 x 4096 x 4096).  With no loads that product would take two thirds of the time, with nothing but loads also: what is left is that the two do not overlap fully.
+// The small tile of 32-bit entries is held to the registers of four waves a SIMD, which its LDS allows and gelu's constants would not.
 template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY>
-__global__ __launch_bounds__(WM * WN * 64) void k_linear_tile(LinearArgs g) {
+__global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 1) void k_linear_tile(LinearArgs g) {
     constexpr int NT = WM * WN * 64, TM = WM * FM * 32, TN = WN * FN * 32;
     constexpr bool FAST = WAY != WAY_REGISTERS;   // whole steps come straight into LDS
     __shared__ chunk_t a0[TM * 8], b0[TN * 8], a1[TM * 8], b1[TN * 8];
@@ -595,7 +604,7 @@ template <int DT, bool WIDE> __global__ __launch_bounds__(FEW_WAVES * 64) void k
     for (int w = 0; w < FEW_WAVES; ++w) v += part[w][i][threadIdx.x & 15];
     if (g.bias) v += g.bias[j];
     if (g.z) store_as(g.z, i * g.ldz + j, DT, v);
-    if (g.act == MLMC_ACT_GELU) v = gelu(v);
+    if (g.act == MLMC_ACT_GELU) v = gelu<DT>(v);
     else if (g.act == MLMC_ACT_RELU) v = relu(v);
     if (g.residual) v += to_f32(((const entry_t<DT>*)g.residual)[i * g.ldr + j]);
     store_as(g.out, i * g.ldo + j, DT, v);

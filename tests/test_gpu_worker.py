@@ -748,3 +748,30 @@ def test_activations_at_infinity(n, m, dtype):
     for kind in ("gelu", "relu"):
         y = P.mlmc_linear(x, one, act=ACT[kind])[:, 0]
         same("y " + kind, y, torch.tensor([float("inf"), 0.0, float("nan"), top, 0.0, 1e30, 0.0, 70.0, 0.0, 0.0], device="cuda").to(DT[dtype]))
+
+
+def test_gelu_of_32_bits_is_as_exact_as_its_roundings():
+    """A product with one is exact, so that only gelu and its slope round.  In units of U and relative to the term: erfc 32 (16 ulp, the most that it may be off), its argument's two roundings
+    2 (z^2 + 1) of the tail; the exponential 6, its argument's z^2 / 2, the products 4.  Near zero, where most entries are, no more than elementary operations with erf are off."""
+    one = torch.ones((1, 1), device="cuda")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    normal = torch.empty(1 << 18, device="cuda").normal_(generator=gen)
+    z = torch.cat((normal, torch.linspace(-12, 12, 100001, device="cuda")))[:, None].contiguous()
+    Z = z.double()
+    phi, density = 0.5 * torch.erfc(-Z / 2 ** 0.5), torch.exp(-0.5 * Z * Z) / (2 * np.pi) ** 0.5
+    tail = U * (35 + 2 * (Z * Z + 1)) * phi
+    for n in (16, z.shape[0]):                                     # the way of few rows and the tiles
+        y = P.mlmc_linear(z[:n], one, act=ACT["gelu"]).double()
+        off = (y - (Z * phi)[:n]).abs() - (tail * Z.abs() + 1e-37)[:n]
+        assert bool((off <= 0).all()), float(off.max())
+    slope = P.mlmc_linear_dgrad(torch.ones_like(z), one, act=ACT["gelu"], z=z).double()
+    want = phi + Z * density
+    off = (slope - want).abs() - (tail + U * (Z * Z / 2 + 10) * (Z * density).abs() + U * want.abs() + 1e-37)
+    assert bool((off <= 0).all()), float(off.max())
+    near_, n = z[:1 << 18], 1 << 18
+    erf = torch.erf(near_ * 0.5 ** 0.5)
+    rms = lambda v: float(v.pow(2).mean().sqrt())  # noqa: E731
+    assert rms(y[:n] - (Z * phi)[:n]) <= rms((0.5 * near_ * (1 + erf)).double() - (Z * phi)[:n])
+    plain = 0.5 * (1 + erf) + near_ * torch.exp(-0.5 * near_ * near_) * (2 * np.pi) ** -0.5
+    assert rms(slope[:n] - want[:n]) <= rms(plain.double() - want[:n])
