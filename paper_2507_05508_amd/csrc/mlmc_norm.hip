@@ -137,7 +137,7 @@ template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG, P <= 8 
 #pragma unroll
         for (int e = 0; e < P; ++e) s += x[e];
         row_sums<T>(s, none, part[odd][0]);
-        const float mean = s * inv_d;
+        const float mean = s / (float)a.d;   // not by the reciprocal: a row of equal entries would not have them as its mean at every width
 #pragma unroll
         for (int e = 0; e < P; ++e) x[e] -= mean;
         of.cut(x);

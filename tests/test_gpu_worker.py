@@ -775,3 +775,14 @@ def test_gelu_of_32_bits_is_as_exact_as_its_roundings():
     assert rms(y[:n] - (Z * phi)[:n]) <= rms((0.5 * near_ * (1 + erf)).double() - (Z * phi)[:n])
     plain = 0.5 * (1 + erf) + near_ * torch.exp(-0.5 * near_ * near_) * (2 * np.pi) ** -0.5
     assert rms(slope[:n] - want[:n]) <= rms(plain.double() - want[:n])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [5, 13, 15, 41, 60, 448, 832, 960, 1920, 2624, 3008, 3264, 3520, 4032, 8064, 13000, 20001])
+def test_layer_norm_of_equal_entries_is_the_bias(d, dtype):
+    """The sums of these entries are exact and so is their quotient by the width: the mean is the entry itself, and the row the bias, at widths too whose reciprocal rounds."""
+    b = torch.arange(d, dtype=torch.float32, device="cuda") % 251
+    for v in (1.0, 2.5, 1000.0):
+        y, stats = P.mlmc_layer_norm(torch.full((3, d), v, dtype=DT[dtype], device="cuda"), None, b, with_stats=True)
+        assert bool((stats[:, 0] == v).all()), (v, stats)
+        assert torch.equal(y, b.to(DT[dtype]).expand(3, d)), v
