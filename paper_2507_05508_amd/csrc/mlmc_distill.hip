@@ -63,24 +63,25 @@ template <int DT, int T> __device__ inline void teacher_load(const DistillArgs& 
     }
 }
 
-// 2^((t - greatest) unit) of the thread's entries, their sum; u becomes (t - greatest) / T.
+// exp((t - greatest) / T) of the thread's entries, their sum; u becomes t - greatest.
 template <int T> __device__ inline float teacher_sum(const DistillArgs& a, const int32_t* at, float* u, float tmax) {
     float sum = 0.f;
     for (int k = threadIdx.x; k < a.top; k += T) {
-        u[k] = (u[k] - tmax) * a.inv_temp;
-        if (at[k] >= 0) sum += expf(u[k]);
+        u[k] -= tmax;
+        if (at[k] >= 0) sum += expf(u[k] * a.inv_temp);
     }
     return sum;
 }
 
-// The thread's part of sum_k q_k (log q_k - log p_{i_k}); u becomes q.
+// The thread's part of sum_k q_k T (log q_k - log p_{i_k}), the loss over T; u becomes q.  With T inside the logarithms nothing is divided by it, and its square, which small ones do not
+// have in fp32, is not needed.
 template <int T> __device__ inline float teacher_loss(const DistillArgs& a, const int32_t* at, float* u, const float* gather, float qsum, float m, float psum) {
-    const float log_q = logf(qsum), log_p = logf(psum);
+    const float logs = a.temp * (logf(psum) - logf(qsum));
     float l = 0.f;
     for (int k = threadIdx.x; k < a.top; k += T) {
-        const float v = u[k], q = at[k] >= 0 ? expf(v) / qsum : 0.f;
+        const float v = u[k], q = at[k] >= 0 ? expf(v * a.inv_temp) / qsum : 0.f;
         u[k] = q;
-        if (q != 0.f) l += q * ((v - log_q) - ((gather[k] - m) * a.inv_temp - log_p));
+        if (q != 0.f) l += q * ((v - (gather[k] - m)) + logs);
     }
     return l;
 }
@@ -232,7 +233,7 @@ template <int DT, int T, int N> __global__ __launch_bounds__(T, N <= 8 ? 8 : 4) 
             float loss = 0.f;
 #pragma unroll 4
             for (int w = 0; w < W; ++w) loss += part[4][w];
-            a.loss[row] = a.temp * a.temp * loss;
+            a.loss[row] = a.temp * loss;
         }
         if (ds && !zero) teacher_gradient<DT, T>(a, ds, at, q, gather, m, coef, c, 0, V);
         if (!zero) return;
@@ -374,7 +375,7 @@ template <int DT> __global__ __launch_bounds__(PART_T) void k_distill_finish(Dis
             float loss = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) loss += part[4][w];
-            a.loss[row] = a.temp * a.temp * loss;
+            a.loss[row] = a.temp * loss;
         }
         if (ds && !zero) teacher_gradient<DT, PART_T>(a, ds, at, q, gather, m, coef, c, first, last);
     }

@@ -786,3 +786,23 @@ def test_layer_norm_of_equal_entries_is_the_bias(d, dtype):
         y, stats = P.mlmc_layer_norm(torch.full((3, d), v, dtype=DT[dtype], device="cuda"), None, b, with_stats=True)
         assert bool((stats[:, 0] == v).all()), (v, stats)
         assert torch.equal(y, b.to(DT[dtype]).expand(3, d)), v
+
+
+@pytest.mark.parametrize("n,v", SHAPES)
+def test_distill_at_temperatures_near_zero(n, v):
+    """The softmaxes are one entry each then, and the loss is T (greatest logit - logit at the teacher's greatest), with the roundings of a difference, a product and q; the squares of
+    these temperatures are no numbers of fp32."""
+    print(f"distill cold n={n} v={v}", flush=True)
+    rng = np.random.default_rng(11)
+    s, s64 = rows(rng, n, v, std=2.0)
+    idx = np.tile(np.array([3, 60, 90]), (n, 1))
+    val = np.tile(np.array([0.5, 2.0, -1.0], dtype=np.float32), (n, 1))
+    for t in (1e-12, 1e-20, 1e-25, 1e-30, 1e-36):
+        t = float(np.float32(t))
+        loss, ds = P.mlmc_distill(s, torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(val).cuda(), temperature=t)
+        want = t * (s64.max(1) - s64[:, 60])
+        near(f"loss {t}", loss, want, 8 * U * want)
+        grad = np.zeros((n, v))
+        grad[np.arange(n), s64.argmax(1)] = t
+        grad[:, 60] -= t
+        near(f"dlogits {t}", ds, grad, 8 * U * np.abs(grad))
