@@ -111,6 +111,12 @@ template <int T> __device__ inline void row_sums(float& a, float& b, float2* par
 // 1 / sqrt v: the instruction where it is exact to an ulp, which leaves out subnormal numbers
 __device__ inline float inverse_root(float v) { return v >= 1.2e-38f ? __builtin_amdgcn_rsqf(v) : 1.0f / sqrtf(v); }
 
+// s / d by the reciprocal of d and what that leaves over, which is exact: a row of equal entries has them as its mean at every width.  (A division took 0.3 us of 19; an infinite sum leaves NaN.)
+__device__ inline float quotient(float s, float d, float inv_d) {
+    const float q = s * inv_d, left = fmaf(-q, d, s);
+    return left == left ? fmaf(left, inv_d, q) : q;
+}
+
 // A workgroup takes WG / T rows at a time, and weight and bias stay in registers from round to round.  The next round's rows are on their way while one is worked on.
 template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG, P <= 8 ? 8 : 4) void k_norm_forward_rows(NormArgs a) {
     using Row = RowChunks<DT, T, P>;
@@ -137,7 +143,7 @@ template <int DT, int T, int P, int WG> __global__ __launch_bounds__(WG, P <= 8 
 #pragma unroll
         for (int e = 0; e < P; ++e) s += x[e];
         row_sums<T>(s, none, part[odd][0]);
-        const float mean = s / (float)a.d;   // not by the reciprocal: a row of equal entries would not have them as its mean at every width
+        const float mean = quotient(s, (float)a.d, inv_d);
 #pragma unroll
         for (int e = 0; e < P; ++e) x[e] -= mean;
         of.cut(x);
