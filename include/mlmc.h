@@ -358,7 +358,8 @@ mlmc_status mlmc_linear_wgrad(const void *dy, int64_t lddy, const void *x, int64
  * Distillation from a teacher's top logits.  Row n has a teacher of `top` entries (index i_k, logit t_k); with T = temperature
  *     q_k = exp(t_k / T) / sum exp(t_k' / T) over the entries,  p_j = exp(s_j / T) / sum exp(s_j' / T) over the vocabulary,
  *     loss_n = T^2 sum_k q_k (log q_k - log p_{i_k}),   dlogits_nj = scale dloss_n T (p_j - sum of the q_k with i_k = j).
- * With one entry and T = 1 this is the cross entropy with label i_1.
+ * With one entry and T = 1 this is the cross entropy with label i_1.  The logarithms are fp32 and multiplied by T^2: at large temperatures the loss is as exact as T^2 times their
+ * rounding (2^-24 of the logarithms), however small it is itself.
  *   logits: dev [rows][vocab];  t_idx, t_val: dev [rows][top], 1 <= top <= MLMC_MAX_TEACHER; entries of an index below 0 are padding (their
  *   t_val is not used).  A row without an entry, or with none above -Inf, is masked: its loss and gradient are 0, whatever its logits.
  *   An index >= vocab makes the row's loss NaN, its gradient 0, and sets MLMC_DEV_RANGE.  A logit of -Inf has p = 0; NaN, +Inf or nothing

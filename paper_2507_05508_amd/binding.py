@@ -347,6 +347,8 @@ def mlmc_message_bits(plan: Plan, msg, bits: Optional[torch.Tensor] = None) -> t
 
 
 # ---- a worker's own step: layer norm, linear layer, distillation loss ------------------------------------------------
+# None of these calls is recorded by autograd: they read the values of their tensors, whether these require gradients or not, what they return requires none, and the gradients
+# are the calls that compute them.
 _DTYPE = {torch.float32: MLMC_F32, torch.bfloat16: MLMC_BF16}
 
 
@@ -415,7 +417,8 @@ def mlmc_distill_workspace(rows: int, vocab: int, top: int) -> int:
 
 def mlmc_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                     y: Optional[torch.Tensor] = None, with_stats: bool = False, stats: Optional[torch.Tensor] = None):
-    """y, or (y, stats) if the statistics for the backward pass are asked for (with_stats, or a tensor [rows, 2] that receives them)."""
+    """y, or (y, stats) if the statistics for the backward pass are asked for (with_stats, or a tensor [rows, 2] that receives them).  Not recorded by autograd: the gradient is
+    mlmc_layer_norm_backward."""
     ldx = _matrix(x, "x")
     dtype = x.dtype
     n, d = x.shape
@@ -463,7 +466,7 @@ def mlmc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional
 def mlmc_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = MLMC_ACT_NONE,
                 residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                 ws: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """y = act(x weight^T + bias) + residual; z, if given, receives what act is applied to."""
+    """y = act(x weight^T + bias) + residual; z, if given, receives what act is applied to.  Not recorded by autograd: the gradients are mlmc_linear_dgrad and mlmc_linear_wgrad."""
     ldx = _matrix(x, "x")
     dtype = x.dtype
     n, k = x.shape
@@ -529,7 +532,7 @@ def mlmc_distill(logits: torch.Tensor, t_idx: torch.Tensor, t_val: torch.Tensor,
                  dloss: Optional[torch.Tensor] = None, scale: float = 1.0, grad: bool = True, loss: Optional[torch.Tensor] = None,
                  dlogits: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """(loss of every row, scale * dloss times its gradient in the logits); the second is None if neither `grad` nor `dlogits` asks for it.
-    dlogits may be the logits themselves.  dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for an index outside the vocabulary."""
+    dlogits may be the logits themselves.  Not recorded by autograd: the gradient is the one returned.  dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for an index outside the vocabulary."""
     ldl = _matrix(logits, "logits")
     dtype = logits.dtype
     n, v = logits.shape

@@ -62,7 +62,9 @@ template <int DT> __device__ inline float gelu(float z) {
 template <int DT> __device__ inline float gelu_slope(float z) {
     float e;
     const float tail = normal_tail<DT>(z, e);
-    const float s = fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228040143268f, e, z > 0.f ? -tail : tail);   // z within +-64 for the same reason; a NaN comes by e
+    const float d = __builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228040143268f;   // z within +-64 for the same reason; a NaN comes by e
+    if constexpr (DT == MLMC_BF16) return fmaf(d, e, z > 0.f ? 1.0f - tail : tail);
+    const float s = fmaf(d, e, z > 0.f ? -tail : tail);   // one rounding less next to 1
     return z > 0.f ? 1.0f + s : s;
 }
 __device__ inline void store_as(void* p, int64_t at, int dtype, float v) {
@@ -656,7 +658,10 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
 }
 // Whether k_linear_few takes a forward product: its workgroups read 16 rows of the weight each, at 30 KB a us by itself and 5 TB/s in all, and with few outputs there are few of them
 // (time of a call, and by tiles in parts: 5 x 512 x 7104 fp32 22.8 us and 17.3, 9 x 295 x 3200 13.4 and 17.7; bf16 1 x 1024 x 4096 7.5 and 14.5, 4 x 256 x 8192 11.8 and 14.9,
-// 16 x 4096 x 4096 10.4 and 11.7, 1 x 8192 x 8192 27.2 and 24.6).
+// 16 x 4096 x 4096 10.4 and 11.7, 1 x 8192 x 8192 27.2 and 24.6).  The costs of tiles have no term for memory, so that beyond those sizes they promise tiles less than the weight's bytes
+// take, and the rule goes to tiles (weights in turn, more than the caches hold; 1 row of 4096 inputs: 11008 outputs 18.8 and 21.6, 14336 23.9 and 25.6, 32000 45.7 and 64.0,
+// 131072 169.6 and 176.4; 16 rows: 26.7 and 22.0, where it stays with the few, 32000 65.4 and 65.7, 131072 251 and 182; 4 x 50021 x 512 16.0 and 12.3, where it stays;
+// fp32 1 x 32000 x 1024 29.0 and 36.9): at one row it gives away up to two fifths, at 16 it is right for the longest.
 static bool few_rows(int64_t I, int64_t J, int64_t C, int dtype) {
     if (I > FEW_ROWS) return false;
     const float row = (float)C * (dtype == MLMC_BF16 ? 2.f : 4.f), alone = 16.f * row / 3.0e4f, all = (float)J * row / 5.0e6f;
@@ -759,7 +764,9 @@ template <bool AA, bool BA> static mlmc_status linear_run(const LinearArgs& g, i
     return dtype == MLMC_F32 ? linear_layout<MLMC_F32, AA, BA>(g, st) : linear_layout<MLMC_BF16, AA, BA>(g, st);
 }
 
-constexpr int64_t LINEAR_ROWS_MAX = (int64_t)1 << 21;   // workgroups of 64 rows along the grid's second axis: under 2^16
+// Sizes go up to this: indices of the contraction, two steps past its end, and numbers of tiles are int, offsets in a tile of copied rows (4 MB each) 32 bits; a product whose matrices fit
+// in memory has at most 2^31 threads.
+constexpr int64_t LINEAR_ROWS_MAX = (int64_t)1 << 21;
 static bool linear_sizes_ok(int64_t n, int64_t m, int64_t k) {
     return n >= 0 && n <= LINEAR_ROWS_MAX && m >= 1 && m <= LINEAR_ROWS_MAX && k >= 1 && k <= LINEAR_ROWS_MAX;
 }

@@ -37,7 +37,6 @@ template <int DT, bool WIDE> __device__ inline chunk_t cut_chunk(chunk_t w, int6
     return __builtin_bit_cast(chunk_t, over >= E || r >= R ? (unsigned __int128)0 : v >> (BITS * (int)over));
 }
 
-
 template <int CTRL, int ROWS> __device__ inline float dpp(float v, float outside) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, outside), __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false));
 }
@@ -72,16 +71,6 @@ template <int WAVES> __device__ inline float group_sum(float v, float* part) {
     float s = part[0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) s += part[w];
-    return s;
-}
-template <int WAVES> __device__ inline float group_max(float v, float* part) {
-    v = wave_max(v);
-    if (WAVES == 1) return v;
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = part[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) s = fmaxf(s, part[w]);
     return s;
 }
 
