@@ -37,9 +37,9 @@ def _quantize(name, rows, width, dtype="bf16", pad=0):
     return {"name": name, "op": "quantize", "rows": rows, "width": width, "dtype": dtype, "pad": pad}
 
 
-def _linear(name, rows, outputs, inputs, dtype="bf16", act="none", residual=False, pad=0):
-    """dtype: of the result and the residual; pad: entries (of 8 bits) behind a row of x."""
-    return {"name": name, "op": "linear_q8", "rows": rows, "outputs": outputs, "inputs": inputs, "dtype": dtype, "act": act,
+def _linear(name, rows, outputs, inputs, act="none", residual=False, pad=0):
+    """Results and residual have 16 bits; pad: entries (of 8 bits) behind a row of x."""
+    return {"name": name, "op": "linear_q8", "rows": rows, "outputs": outputs, "inputs": inputs, "dtype": "bf16", "act": act,
             "residual": residual, "pad": pad}
 
 
@@ -98,7 +98,7 @@ def draw(rng):
     if op == "linear_q8":
         outputs, inputs = _size(rng, 128, 8192), _size(rng, 128, 8192)
         rows = _size(rng, 1, max(1, min(16384, MOST_PRODUCT // (outputs * inputs))))
-        c = _linear("", rows, outputs, inputs, dtype, rng.choice(ACTS), rng.random() < 0.5, rng.choice((0, 0, 5, 16)))
+        c = _linear("", rows, outputs, inputs, rng.choice(ACTS), rng.random() < 0.5, rng.choice((0, 0, 5, 16)))
     elif op == "logprobs":
         vocab = _size(rng, 1000, 262144)
         rows = _size(rng, 1, min(8192, MOST_LOGITS // vocab // (2 if dtype == "f32" else 1)))
@@ -321,8 +321,7 @@ def _own(s, case):
         return {"q": q, "scale": scale}
     if op == "linear_q8":
         act = {"none": P.MLMC_ACT_NONE, "relu": P.MLMC_ACT_RELU, "gelu": P.MLMC_ACT_GELU}[case["act"]]
-        return {"y": P.mlmc_linear_q8(s["x"], s["x_scale"], s["weight"], s["weight_scale"], s["bias"], act=act, residual=s["residual"],
-                                      dtype=DTYPES[case["dtype"]])}
+        return {"y": P.mlmc_linear_q8(s["x"], s["x_scale"], s["weight"], s["weight_scale"], s["bias"], act=act, residual=s["residual"])}
     if op == "dropout":
         return {"y": P.mlmc_dropout(s["x"], case["p"], s["seed"], s["step"], stream=s["stream"], residual=s["residual"])}
     if case["backward"]:
