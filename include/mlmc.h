@@ -55,7 +55,7 @@ typedef enum {
 #define MLMC_DEV_CAPACITY 1  /* row_off[M] > capacity: entries past capacity were not written */
 #define MLMC_DEV_NONFINITE 2 /* an Inf or NaN input was seen (it is ordered by its bit pattern) */
 #define MLMC_DEV_INTERNAL 4  /* an internal consistency check failed (counts do not add up) */
-#define MLMC_DEV_RANGE 16    /* mlmc_distill: a teacher's index is not below the vocabulary */
+#define MLMC_DEV_RANGE 16    /* mlmc_distill, mlmc_token_logprobs: a teacher's index or a token is not below the vocabulary */
 #define MLMC_DEV_REDONE 8    /* not an error: a row's sampled threshold search was refuted and the row was redone exactly */
 
 typedef enum { MLMC_F32 = 0, MLMC_BF16 = 1 } mlmc_dtype;
@@ -68,6 +68,7 @@ typedef enum { MLMC_ACT_NONE = 0, MLMC_ACT_RELU = 1, MLMC_ACT_GELU = 2 } mlmc_ac
 #define MLMC_MAX_SLEVELS 65536 /* MLMC_STOPK: L = ceil(d / s) <= 65536 */
 #define MLMC_MAX_RTN_LEVELS 8  /* MLMC_RTN: L <= 8 */
 #define MLMC_MAX_TEACHER 1024  /* mlmc_distill: entries of a row's teacher */
+#define MLMC_MAX_ANSWERS 128   /* tokens, and alternatives, of a row of mlmc_token_logprobs */
 #define MLMC_TILE 4096       /* elements per tile of the per-row offset table */
 
 /*
@@ -290,8 +291,8 @@ mlmc_status mlmc_aggregate_update(const mlmc_plan_t *plan, const int32_t *level,
 mlmc_status mlmc_message_bits(const mlmc_plan_t *plan, const int32_t *level, uint64_t *bits, void *hip_stream);
 
 /*
- * What a worker computes before it has a gradient: layer norm, the linear layer, the distillation loss, each with its
- * gradient.  They need no plan.  Weight gradients are written in fp32 or bf16 (grad_dtype) at any place that is aligned to an entry, so
+ * What a worker computes before it has a gradient: layer norm and root-mean-square norm, the linear layer, dropout, the distillation loss and the
+ * log probabilities of tokens, each with its gradient; and what its teacher answers with, in 8 bits.  They need no plan.  Weight gradients are written in fp32 or bf16 (grad_dtype) at any place that is aligned to an entry, so
  * that a worker's tensors can lie one behind the other in its row of the matrix g that the compress calls read.
  * Conventions beside those at the top:
  *   - A matrix is row-major with the row distance given behind its pointer (in entries, at least its width); rows need no alignment beyond
@@ -371,6 +372,86 @@ size_t mlmc_distill_workspace(int64_t rows, int64_t vocab, int top);
 mlmc_status mlmc_distill(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const int32_t *t_idx, const float *t_val, int top,
                          float temperature, const float *dloss, float scale, float *loss, void *dlogits, int64_t ldd, int32_t *dev_status,
                          void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Root-mean-square norm of every row of s = x + residual: y_j = s_j r weight_j, r = 1 / sqrt(mean s^2 + eps).
+ *   x: dev [rows][ldx];  residual: dev [rows][ldr] or NULL (s = x);  weight: dev [d] fp32 or NULL (1);  eps >= 0;
+ *   sum: dev [rows][lds] (out) or NULL: receives s; only with a residual;  y: dev [rows][ldy] (out) or NULL;
+ *   q, scale: dev [rows][ldq] bytes and [rows] fp32 (out), or both NULL: y in 8 bits as mlmc_quantize has it;  at least one of y and q;
+ *   rstd: dev [rows] fp32 (out) or NULL: r, for the backward pass.  sum and y may each be x or the residual (not both the same).
+ * The sum of the squares is fp32: of rows for which it is infinite r is 0, and y the product with that.
+ */
+mlmc_status mlmc_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int64_t rows, int64_t d, int dtype, const float *weight, float eps,
+                          void *sum, int64_t lds, void *y, int64_t ldy, uint8_t *q, int64_t ldq, float *scale, float *rstd, void *hip_stream);
+
+/*
+ * Its gradient.  With h_j = s_j r and c_j = dy_j weight_j: ds_j = r (c_j - h_j mean(c h)) + residual_j, which is the gradient of x and of the residual
+ * alike; dweight_j = sum over rows of dy_j h_j.
+ *   dy: dev [rows][lddy], the gradient of y (of its unrounded values, where they went on in 8 bits);  s: dev [rows][lds]: the sum that the forward call stored, or x;
+ *   rstd: as mlmc_rms_norm wrote it;  residual: dev [rows][ldr] or NULL: a gradient that comes to s by another way;
+ *   dx: dev [rows][lddx] (out; may be dy, s or residual);  dweight: dev [d] of grad_dtype (out) or NULL (ws is not needed then).
+ */
+size_t mlmc_rms_norm_workspace(int64_t rows, int64_t d);
+mlmc_status mlmc_rms_norm_backward(const void *dy, int64_t lddy, const void *s, int64_t lds, int64_t rows, int64_t d, int dtype, const float *weight, const float *rstd,
+                                   const void *residual, int64_t ldr, void *dx, int64_t lddx, void *dweight, int grad_dtype, void *ws, size_t ws_bytes,
+                                   void *hip_stream);
+
+/*
+ * Rows in 8 bits (e4m3: sign, 4 exponent bits of bias 7, 3 bits behind the point, greatest value 448, one NaN and no infinity):
+ * scale = max_j |x_j| / 448, at least 2^-100; q_j = the e4m3 value nearest to x_j / scale, ties to even.  q_j stands for q_j scale.
+ *   x: dev [rows][ldx];  q: dev [rows][ldq] bytes (out);  scale: dev [rows] fp32 (out).
+ *   A row that holds a NaN or an infinity has the scale NaN and nothing but NaN.
+ */
+mlmc_status mlmc_quantize(const void *x, int64_t ldx, int64_t rows, int64_t d, int dtype, uint8_t *q, int64_t ldq, float *scale, void *hip_stream);
+
+/*
+ * Linear layer of matrices in 8 bits, a teacher's forward pass: v = (x_scale_n w_scale_m) (x_n . weight_m) + bias, y = act(v) + residual.
+ *   x: dev [rows][ldx] bytes, x_scale: dev [rows] fp32;  weight: dev [outputs][ldw] bytes, w_scale: dev [outputs] fp32: as mlmc_quantize and mlmc_rms_norm write them
+ *   (any other scales, too);  bias: dev [outputs] fp32 or NULL;  residual: dev [rows][ldr] bf16 or NULL;  y: dev [rows][ldy] bf16 (out; may be residual).
+ *   0 <= rows, 1 <= outputs, inputs, each at most 2^21.
+ * The matrix units add products in groups and cut what lies more than 12 binary places below the greatest of a group, before the fp32 sum (about 1.5e-5 of a
+ * result of normal entries); results have 16 bits for that reason.  Rows whose starts and distances are multiples of 16 bytes are the fastest.
+ */
+size_t mlmc_linear_q8_workspace(int64_t rows, int64_t outputs, int64_t inputs);
+mlmc_status mlmc_linear_q8(const uint8_t *x, int64_t ldx, const float *x_scale, const uint8_t *weight, int64_t ldw, const float *w_scale, int64_t rows, int64_t outputs,
+                           int64_t inputs, const float *bias, int act, const void *residual, int64_t ldr, void *y, int64_t ldy, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Dropout whose mask is not stored: y_ij = x_ij / (1 - p) where the entry is kept and 0 where it is not, plus residual_ij.  Its gradient is the same call on the gradient
+ * of y, with the same p, seed, step, stream and row0, and as residual a gradient that comes by another way, or none.
+ *   p is taken to the nearest multiple of 2^-16 (below 1; MLMC_EINVAL if that is 1), t = p 2^16.  Entry (i, j) is kept if half j % 8 of Philox4x32-10 with key = (seed_lo, seed_hi) and
+ *   counter = (step, stream, row0 + i, 1 + j / 8) is at least t, halves of 16 bits counted from the low one of word 0: a function of the entry's place alone, whatever
+ *   type and strides.  The level draws have 0 in the last word of the counter, so that they may use the same seed and step.
+ *   step < 2^32;  stream: tells apart the dropouts of a step (a worker's layers);  0 <= row0, row0 + rows <= 2^32: the first row's number, for matrices cut into parts.
+ *   x: dev [rows][ldx];  residual: dev [rows][ldr] or NULL;  y: dev [rows][ldy] (out; may be x or residual).  What is dropped leaves nothing, infinities and NaN too.
+ */
+mlmc_status mlmc_dropout(const void *x, int64_t ldx, int64_t rows, int64_t d, int dtype, double p, uint64_t seed, uint64_t step, uint32_t stream, int64_t row0,
+                         const void *residual, int64_t ldr, void *y, int64_t ldy, void *hip_stream);
+
+/*
+ * Log probabilities of given tokens, entropy and the top alternatives of every row of logits; with T = temperature log p_j = s_j / T - log sum exp(s_j' / T).
+ *   logits: dev [rows][ldl], vocab <= 2^21;  tokens: dev [rows][given], 0 <= given <= MLMC_MAX_ANSWERS: a token below 0 is padding, its log probability is 0; one >= vocab
+ *   makes it NaN and sets MLMC_DEV_RANGE;  logprob: dev [rows][given] fp32 (out);  entropy: dev [rows] fp32 (out) or NULL: -sum p_j log p_j;
+ *   top_idx, top_logprob: dev [rows][top] (out), 0 <= top <= MLMC_MAX_ANSWERS: the entries of the greatest logits in descending order, of equal ones the lowest index first, and their log
+ *   probabilities.  A logit of -Inf has p = 0 and is no alternative: places without one have index -1 and -Inf.  With T = 1 these are a teacher's entries for mlmc_distill, at any
+ *   temperature there, since its softmax takes log probabilities as it takes logits.
+ *   stats: dev [rows][3] fp32 (out) or NULL: greatest logit, log of the sum of exp((s - greatest) / T), entropy, for the backward pass.
+ *   Rows with NaN, +Inf or nothing but -Inf: log probabilities (but those of padding), entropy and top_logprob are NaN, the indices -1.
+ */
+size_t mlmc_token_logprobs_workspace(int64_t rows, int64_t vocab, int top);
+mlmc_status mlmc_token_logprobs(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const int32_t *tokens, int given, int top, float temperature,
+                                float *logprob, float *entropy, int32_t *top_idx, float *top_logprob, float *stats, int32_t *dev_status, void *ws, size_t ws_bytes,
+                                void *hip_stream);
+
+/*
+ * Its gradient in the logits: dlogits_j = (sum of the g_k of the tokens and alternatives that are j - p_j sum_k g_k - dentropy p_j (log p_j + entropy)) / T, g_k = dlogprob and dtop.
+ *   stats: as mlmc_token_logprobs wrote it for these logits and this temperature;  tokens, dlogprob: dev [rows][given];  top_idx, dtop: dev [rows][top];  tokens outside the vocabulary
+ *   (padding, or an alternative that is not there) are left out, with their g;  dentropy: dev [rows] or NULL (0);  dlogits: dev [rows][ldd] (out; may be logits).
+ *   A row whose g_k and dentropy are all 0 has gradient 0, whatever its logits.
+ */
+mlmc_status mlmc_token_logprobs_backward(const void *logits, int64_t ldl, int64_t rows, int64_t vocab, int dtype, const float *stats, const int32_t *tokens, int given,
+                                         const float *dlogprob, const int32_t *top_idx, int top, const float *dtop, const float *dentropy, float temperature, void *dlogits,
+                                         int64_t ldd, void *hip_stream);
 
 /*
  * Per-kernel timing for benchmarks (measurement aid, not part of the method).  While enabled, every kernel

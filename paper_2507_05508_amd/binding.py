@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -24,13 +24,15 @@ MLMC_TOPK, MLMC_BITS, MLMC_FBITS, MLMC_STOPK, MLMC_VBITS, MLMC_RTN = 0, 1, 2, 3,
 MLMC_ACT_NONE, MLMC_ACT_RELU, MLMC_ACT_GELU = 0, 1, 2
 MLMC_MAX_SLEVELS = 65536
 MLMC_MAX_TEACHER = 1024
+MLMC_MAX_ANSWERS = 128
 MLMC_TILE = 4096
 MLMC_MAX_LEVELS = 32
 
 EXPORTS = ["mlmc_plan", "mlmc_plan_destroy", "mlmc_plan_set_sampling", "mlmc_plan_set_staging", "mlmc_plan_set_overlap", "mlmc_plan_num_tiles", "mlmc_plan_chunk", "mlmc_plan_num_planes", "mlmc_geometric_p",
            "mlmc_status_string", "mlmc_level_norms", "mlmc_compress_topk", "mlmc_compress_bits", "mlmc_compress_bits_static", "mlmc_compress_rtn", "mlmc_aggregate", "mlmc_aggregate_update", "mlmc_message_bits",
            "mlmc_layer_norm", "mlmc_layer_norm_workspace", "mlmc_layer_norm_backward", "mlmc_linear", "mlmc_linear_workspace", "mlmc_linear_dgrad", "mlmc_linear_wgrad",
-           "mlmc_distill", "mlmc_distill_workspace",
+           "mlmc_distill", "mlmc_distill_workspace", "mlmc_rms_norm", "mlmc_rms_norm_workspace", "mlmc_rms_norm_backward", "mlmc_quantize", "mlmc_linear_q8", "mlmc_linear_q8_workspace",
+           "mlmc_dropout", "mlmc_token_logprobs", "mlmc_token_logprobs_workspace", "mlmc_token_logprobs_backward",
            "mlmc_profile_enable", "mlmc_profile_reset", "mlmc_profile_num_kernels", "mlmc_profile_kernel_name",
            "mlmc_profile_get"]
 
@@ -87,7 +89,8 @@ def lib():
         L.mlmc_message_bits.restype = C.c_int
         L.mlmc_message_bits.argtypes = [vp, vp, vp, vp]
         f32, sz = C.c_float, C.c_size_t
-        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64, i32, i32]), ("mlmc_distill_workspace", [i64, i64, i32])):
+        for name, args in (("mlmc_layer_norm_workspace", [i64, i64]), ("mlmc_linear_workspace", [i64, i64, i64, i32, i32]), ("mlmc_distill_workspace", [i64, i64, i32]),
+                           ("mlmc_rms_norm_workspace", [i64, i64]), ("mlmc_linear_q8_workspace", [i64, i64, i64]), ("mlmc_token_logprobs_workspace", [i64, i64, i32])):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = args
         for name, args in (("mlmc_layer_norm", [vp, i64, i64, i64, i32, vp, vp, f32, vp, i64, vp, vp]),
@@ -95,7 +98,14 @@ def lib():
                            ("mlmc_linear", [vp, i64, vp, i64, i64, i64, i64, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, sz, vp]),
                            ("mlmc_linear_dgrad", [vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, sz, vp]),
                            ("mlmc_linear_wgrad", [vp, i64, vp, i64, i64, i64, i64, i32, vp, i64, vp, i32, vp, sz, vp]),
-                           ("mlmc_distill", [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, f32, vp, vp, i64, vp, vp, sz, vp])):
+                           ("mlmc_distill", [vp, i64, i64, i64, i32, vp, vp, i32, f32, vp, f32, vp, vp, i64, vp, vp, sz, vp]),
+                           ("mlmc_rms_norm", [vp, i64, vp, i64, i64, i64, i32, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp, vp]),
+                           ("mlmc_rms_norm_backward", [vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, i64, vp, i64, vp, i32, vp, sz, vp]),
+                           ("mlmc_quantize", [vp, i64, i64, i64, i32, vp, i64, vp, vp]),
+                           ("mlmc_linear_q8", [vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i32, vp, i64, vp, i64, vp, sz, vp]),
+                           ("mlmc_dropout", [vp, i64, i64, i64, i32, C.c_double, u64, u64, C.c_uint32, i64, vp, i64, vp, i64, vp]),
+                           ("mlmc_token_logprobs", [vp, i64, i64, i64, i32, vp, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+                           ("mlmc_token_logprobs_backward", [vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, i32, vp, vp, f32, vp, i64, vp])):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = args
         L.mlmc_profile_enable.restype = None
@@ -346,7 +356,7 @@ def mlmc_message_bits(plan: Plan, msg, bits: Optional[torch.Tensor] = None) -> t
 
 
 
-# ---- a worker's own step: layer norm, linear layer, distillation loss ------------------------------------------------
+# ---- a worker's own step and its teacher: norms, linear layers, dropout, distillation loss, log probabilities of tokens --
 # None of these calls is recorded by autograd: they read the values of their tensors, whether these require gradients or not, what they return requires none, and the gradients
 # are the calls that compute them.
 _DTYPE = {torch.float32: MLMC_F32, torch.bfloat16: MLMC_BF16}
@@ -553,3 +563,242 @@ def mlmc_distill(logits: torch.Tensor, t_idx: torch.Tensor, t_val: torch.Tensor,
     if rc:
         _check(rc, "mlmc_distill")
     return loss, dlogits
+
+
+class RmsNorm(NamedTuple):
+    """What mlmc_rms_norm was asked for; None in the other places."""
+    y: Optional[torch.Tensor]
+    sum: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+    q: Optional[torch.Tensor]
+    scale: Optional[torch.Tensor]
+
+
+class TokenLogprobs(NamedTuple):
+    """What mlmc_token_logprobs was asked for; None in the other places."""
+    logprob: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_idx: Optional[torch.Tensor]
+    top_logprob: Optional[torch.Tensor]
+    stats: Optional[torch.Tensor]
+
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def _eight_bits(n: int, d: int, like: torch.Tensor) -> torch.Tensor:
+    """A matrix of 8 bits whose rows begin at multiples of 16 bytes, which the product of such matrices reads fastest."""
+    ld = (d + 15) // 16 * 16
+    q = torch.empty((n, ld), dtype=_E4M3, device=like.device)
+    return q if ld == d else q[:, :d]
+
+
+def _or_none(t: Optional[torch.Tensor], name: str, dtype, n: int, d: int):
+    """Address and row distance of a matrix that may be absent."""
+    return (None, 0) if t is None else (t.data_ptr(), _matrix(t, name, dtype, n, d))
+
+
+@functools.lru_cache(maxsize=4096)
+def mlmc_rms_norm_workspace(rows: int, d: int) -> int:
+    return lib().mlmc_rms_norm_workspace(rows, d)
+
+
+@functools.lru_cache(maxsize=4096)
+def mlmc_linear_q8_workspace(rows: int, outputs: int, inputs: int) -> int:
+    return lib().mlmc_linear_q8_workspace(rows, outputs, inputs)
+
+
+@functools.lru_cache(maxsize=4096)
+def mlmc_token_logprobs_workspace(rows: int, vocab: int, top: int) -> int:
+    return lib().mlmc_token_logprobs_workspace(rows, vocab, top)
+
+
+def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  with_y: bool = True, with_rstd: bool = False, with_q: bool = False, y: Optional[torch.Tensor] = None,
+                  sum: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                  scale: Optional[torch.Tensor] = None) -> RmsNorm:
+    """The norm of x + residual: in x's type (y), in 8 bits (q, float8_e4m3fn, and the scale of every row), or both; with a residual the sum as well.  Tensors that are given receive
+    what is asked for.  Not recorded by autograd: the gradient is mlmc_rms_norm_backward."""
+    ldx = _matrix(x, "x")
+    dtype = x.dtype
+    n, d = x.shape
+    p_r, ldr = _or_none(residual, "residual", dtype, n, d)
+    if residual is None:
+        if sum is not None:
+            raise MlmcError("sum is an output of a norm with a residual")
+    elif sum is None:
+        sum = x.new_empty((n, d))
+    if y is None and with_y:
+        y = x.new_empty((n, d))
+    if q is None and with_q:
+        q = _eight_bits(n, d, x)
+    if q is not None and scale is None:
+        scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    if q is None and scale is not None:
+        raise MlmcError("scale is that of q")
+    if y is None and q is None:
+        raise MlmcError("neither y nor q is asked for")
+    if rstd is None and with_rstd:
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    p_s, lds = _or_none(sum, "sum", dtype, n, d)
+    p_y, ldy = _or_none(y, "y", dtype, n, d)
+    p_q, ldq = _or_none(q, "q", _E4M3, n, d)
+    rc = lib().mlmc_rms_norm(x.data_ptr(), ldx, p_r, ldr, n, d, _DTYPE[dtype], _vector(weight, "weight", d), eps, p_s, lds, p_y, ldy, p_q, ldq,
+                             _vector(scale, "scale", n), _vector(rstd, "rstd", n), _stream())
+    if rc:
+        _check(rc, "mlmc_rms_norm")
+    return RmsNorm(y, sum, rstd, q, scale)
+
+
+def mlmc_rms_norm_backward(dy: torch.Tensor, s: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor, dweight: Optional[torch.Tensor] = None,
+                           residual: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of x and of the forward call's residual alike; s: the sum that the forward call stored (x where there was none); residual: a gradient that comes to the sum by
+    another way; dweight ([d], fp32 or bf16, for instance a part of a row of the gradient matrix) is written in place."""
+    lds = _matrix(s, "s")
+    dtype = s.dtype
+    n, d = s.shape
+    if dx is None:
+        dx, lddx = s.new_empty((n, d)), d
+    else:
+        lddx = _matrix(dx, "dx", dtype, n, d)
+    g, need = torch.float32, 0
+    if dweight is not None:
+        g = dweight.dtype
+        if g not in _DTYPE:
+            raise MlmcError("dweight must be of float32 or bfloat16")
+        need = mlmc_rms_norm_workspace(n, d)
+    p, nbytes, ws = _scratch(ws, need, s)
+    p_r, ldr = _or_none(residual, "residual", dtype, n, d)
+    if rstd is None:
+        raise MlmcError("the gradient needs rstd")
+    rc = lib().mlmc_rms_norm_backward(dy.data_ptr(), _matrix(dy, "dy", dtype, n, d), s.data_ptr(), lds, n, d, _DTYPE[dtype], _vector(weight, "weight", d),
+                                      _vector(rstd, "rstd", n), p_r, ldr, dx.data_ptr(), lddx, _vector(dweight, "dweight", d, g), _DTYPE[g], p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_rms_norm_backward")
+    return dx
+
+
+def mlmc_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """(q, scale): the rows of x in 8 bits (float8_e4m3fn) and the scale of every row."""
+    ldx = _matrix(x, "x")
+    n, d = x.shape
+    if q is None:
+        q = _eight_bits(n, d, x)
+    if scale is None:
+        scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    rc = lib().mlmc_quantize(x.data_ptr(), ldx, n, d, _DTYPE[x.dtype], q.data_ptr(), _matrix(q, "q", _E4M3, n, d), _vector(scale, "scale", n), _stream())
+    if rc:
+        _check(rc, "mlmc_quantize")
+    return q, scale
+
+
+def mlmc_linear_q8(x: torch.Tensor, x_scale: torch.Tensor, weight: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                   act: int = MLMC_ACT_NONE, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                   ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = act(x weight^T + bias) + residual in bfloat16, x and weight in 8 bits (float8_e4m3fn) with a scale for every row, as mlmc_rms_norm and mlmc_quantize give them."""
+    ldx = _matrix(x, "x", _E4M3)
+    n, k = x.shape
+    ldw = _matrix(weight, "weight", _E4M3, -1, k)
+    m = weight.shape[0]
+    if x_scale is None or w_scale is None:
+        raise MlmcError("matrices in 8 bits need their scales")
+    if y is None:
+        y, ldy = torch.empty((n, m), dtype=torch.bfloat16, device=x.device), m
+    else:
+        ldy = _matrix(y, "y", torch.bfloat16, n, m)
+    p, nbytes, ws = _scratch(ws, mlmc_linear_q8_workspace(n, m, k), x)
+    p_r, ldr = _or_none(residual, "residual", torch.bfloat16, n, m)
+    rc = lib().mlmc_linear_q8(x.data_ptr(), ldx, _vector(x_scale, "x_scale", n), weight.data_ptr(), ldw, _vector(w_scale, "w_scale", m), n, m, k,
+                              _vector(bias, "bias", m), act, p_r, ldr, y.data_ptr(), ldy, p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_linear_q8")
+    return y
+
+
+def mlmc_dropout(x: torch.Tensor, p: float, seed: int, step: int, stream: int = 0, row0: int = 0, residual: Optional[torch.Tensor] = None,
+                 y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """What is kept of x, over 1 - p, plus residual; the mask is a function of (seed, step, stream, row0 + row, column) and is not stored.  Not recorded by autograd: the gradient is the
+    same call on the gradient of y, with the same numbers.  seed is taken modulo 2^64."""
+    ldx = _matrix(x, "x")
+    dtype = x.dtype
+    n, d = x.shape
+    if y is None:
+        y, ldy = x.new_empty((n, d)), d
+    else:
+        ldy = _matrix(y, "y", dtype, n, d)
+    if not (0 <= step < 1 << 32 and 0 <= stream < 1 << 32 and 0 <= row0 <= 1 << 32):
+        raise MlmcError("step, stream and row0 are numbers of 32 bits")
+    p_r, ldr = _or_none(residual, "residual", dtype, n, d)
+    rc = lib().mlmc_dropout(x.data_ptr(), ldx, n, d, _DTYPE[dtype], p, seed, step, stream, row0, p_r, ldr, y.data_ptr(), ldy, _stream())
+    if rc:
+        _check(rc, "mlmc_dropout")
+    return y
+
+
+def mlmc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0, with_entropy: bool = False,
+                        with_stats: bool = False, dev_status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> TokenLogprobs:
+    """Log probabilities of the tokens (int32 [rows] or [rows, given], -1: padding), the entropy and the `top` alternatives of every row, whose indices and log probabilities
+    mlmc_distill takes as a teacher's entries.  Not recorded by autograd: the gradient is mlmc_token_logprobs_backward, which needs the stats.
+    dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for a token outside the vocabulary."""
+    ldl = _matrix(logits, "logits")
+    n, v = logits.shape
+    at = logits.device
+    given, p_t, logprob = 0, None, None
+    if tokens is not None:
+        given = _given(tokens)
+        p_t = _table(tokens if tokens.dim() == 2 else tokens.unsqueeze(1), "tokens", n, given, torch.int32)
+        logprob = torch.empty(tokens.shape, dtype=torch.float32, device=at)
+    entropy = torch.empty(n, dtype=torch.float32, device=at) if with_entropy else None
+    stats = torch.empty((n, 3), dtype=torch.float32, device=at) if with_stats else None
+    top_idx = top_logprob = None
+    if top > 0:
+        top_idx = torch.empty((n, top), dtype=torch.int32, device=at)
+        top_logprob = torch.empty((n, top), dtype=torch.float32, device=at)
+    p, nbytes, ws = _scratch(ws, mlmc_token_logprobs_workspace(n, v, top), logits)
+    rc = lib().mlmc_token_logprobs(logits.data_ptr(), ldl, n, v, _DTYPE[logits.dtype], p_t, given, top, temperature,
+                                   None if logprob is None else logprob.data_ptr(), None if entropy is None else entropy.data_ptr(),
+                                   None if top_idx is None else top_idx.data_ptr(), None if top_logprob is None else top_logprob.data_ptr(),
+                                   None if stats is None else stats.data_ptr(), _vector(dev_status, "dev_status", 1, torch.int32), p, nbytes, _stream())
+    if rc:
+        _check(rc, "mlmc_token_logprobs")
+    return TokenLogprobs(logprob, entropy, top_idx, top_logprob, stats)
+
+
+def _given(tokens: torch.Tensor) -> int:
+    if tokens.dim() not in (1, 2):
+        raise MlmcError("tokens must be a vector or a matrix")
+    return tokens.shape[1] if tokens.dim() == 2 else 1
+
+
+def mlmc_token_logprobs_backward(logits: torch.Tensor, stats: torch.Tensor, tokens: Optional[torch.Tensor] = None, dlogprob: Optional[torch.Tensor] = None,
+                                 top_idx: Optional[torch.Tensor] = None, dtop: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None,
+                                 temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient in the logits of what mlmc_token_logprobs returned for them: dlogprob that of the tokens' log probabilities, dtop of the alternatives', dentropy of the entropies.
+    dlogits may be the logits themselves."""
+    ldl = _matrix(logits, "logits")
+    dtype = logits.dtype
+    n, v = logits.shape
+    if (tokens is None) != (dlogprob is None) or (top_idx is None) != (dtop is None):
+        raise MlmcError("tokens and dlogprob, top_idx and dtop come together")
+    given = top = 0
+    p_t = p_g = p_i = p_a = None
+    if tokens is not None:
+        given = _given(tokens)
+        if dlogprob.shape != tokens.shape:
+            raise MlmcError("dlogprob has the size of tokens")
+        p_t = _table(tokens if tokens.dim() == 2 else tokens.unsqueeze(1), "tokens", n, given, torch.int32)
+        p_g = _table(dlogprob if dlogprob.dim() == 2 else dlogprob.unsqueeze(1), "dlogprob", n, given, torch.float32)
+    if top_idx is not None:
+        if top_idx.dim() != 2:
+            raise MlmcError("top_idx must be a matrix")
+        top = top_idx.shape[1]
+        p_i, p_a = _table(top_idx, "top_idx", n, top, torch.int32), _table(dtop, "dtop", n, top, torch.float32)
+    if dlogits is None:
+        dlogits, ldd = logits.new_empty((n, v)), v
+    else:
+        ldd = _matrix(dlogits, "dlogits", dtype, n, v)
+    rc = lib().mlmc_token_logprobs_backward(logits.data_ptr(), ldl, n, v, _DTYPE[dtype], _table(stats, "stats", n, 3, torch.float32), p_t, given, p_g, p_i, top, p_a,
+                                            _vector(dentropy, "dentropy", n), temperature, dlogits.data_ptr(), ldd, _stream())
+    if rc:
+        _check(rc, "mlmc_token_logprobs_backward")
+    return dlogits

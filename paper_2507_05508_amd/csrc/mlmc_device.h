@@ -268,8 +268,7 @@ __device__ __forceinline__ void stream_slice(const RowLoader<DT, true>& ld, int6
 }
 
 // ---- Philox4x32-10 (Salmon et al., SC'11), from the published round function ----------------------
-__device__ __forceinline__ uint32_t philox_word0(uint64_t seed, uint64_t step, uint32_t worker) {
-    uint32_t c0 = (uint32_t)step, c1 = (uint32_t)(step >> 32), c2 = worker, c3 = 0u;
+__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint64_t seed) {
     uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
@@ -286,8 +285,10 @@ __device__ __forceinline__ uint32_t philox_word0(uint64_t seed, uint64_t step, u
         c0 = n0;
         c2 = n2;
     }
-    return c0;
+    return make_uint4(c0, c1, c2, c3);
 }
+// the one word of a worker's step
+__device__ __forceinline__ uint32_t philox_word0(uint64_t seed, uint64_t step, uint32_t worker) { return philox((uint32_t)step, (uint32_t)(step >> 32), worker, 0u, seed).x; }
 
 // Level draw shared by the Top-k and bit-wise paths: integer inverse CDF of one 32-bit uniform.
 // p: L probabilities (local array).  Returns the level in 1..L.

@@ -38,8 +38,6 @@ struct DistillArgs {
 
 __global__ void k_distill_clear(int32_t* dev_status) { *dev_status = 0; }
 
-__device__ inline float power(float x, float unit) { return __builtin_amdgcn_exp2f(x * unit); }   // x is a difference: scaled before it is taken, large logits would lose it
-
 constexpr int T_LIVE = 1, T_BAD = 2;
 
 // The teacher's entries of a row into LDS (index -1: padding, also up to a multiple of four) and, with them, the logits at their places; a thread's greatest value and what it has seen.
@@ -103,40 +101,6 @@ template <int DT, int T> __device__ inline void teacher_gradient(const DistillAr
             qs += w.w == i ? v.w : 0.f;
         }
         ds[i] = from_f32<DT>(fmaf(power(gather[k] - m, a.unit), coef, -c * qs));
-    }
-}
-
-// A thread's chunk of 16 bytes of a row as floats; -Inf past the end.
-template <int DT> __device__ inline void chunk_floats(float (&f)[DT == MLMC_BF16 ? 8 : 4], chunk_t v) {
-    if constexpr (DT == MLMC_BF16) {
-        const v8b u = __builtin_bit_cast(v8b, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (float)u[e];
-    } else {
-        const v4f u = __builtin_bit_cast(v4f, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = u[e];
-    }
-}
-template <int DT> __device__ inline chunk_t load_chunk(const entry_t<DT>* s, int64_t col, int64_t end) {
-    constexpr int E = DT == MLMC_BF16 ? 8 : 4;
-    if (col + E <= end) return *(const chunk_u*)(s + col);
-    entry_t<DT> __attribute__((ext_vector_type(E))) u;
-#pragma unroll
-    for (int e = 0; e < E; ++e) u[e] = col + e < end ? s[col + e] : (entry_t<DT>)-INFINITY;
-    return __builtin_bit_cast(chunk_t, u);
-}
-template <int DT> __device__ inline void store_chunk(entry_t<DT>* s, int64_t col, int64_t end, const float (&f)[DT == MLMC_BF16 ? 8 : 4]) {
-    constexpr int E = DT == MLMC_BF16 ? 8 : 4;
-    if (col + E <= end) {
-        entry_t<DT> __attribute__((ext_vector_type(E))) u;
-#pragma unroll
-        for (int e = 0; e < E; ++e) u[e] = (entry_t<DT>)f[e];
-        *(chunk_u*)(s + col) = __builtin_bit_cast(chunk_t, u);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (col + e < end) s[col + e] = (entry_t<DT>)f[e];
     }
 }
 

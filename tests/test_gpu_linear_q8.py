@@ -1,0 +1,119 @@
+"""The linear layer of 8-bit matrices on the GPU.
+
+To the bit: entries of small whole numbers have products of at most 16 and at least 1, which the matrix units add exactly (they cut what is 2^-12 of the greatest of a group), sums below 2^24
+and scales that are powers of two: the result is the exact one, rounded once to 16 bits.  Of normal entries: a product loses less than 2^-12 of the greatest of its group, which for normal entries
+is below three times their mean square; independent cuts add up like the products themselves, so that the relative 2-norm of what is cut is below 3 / sqrt(3) 2^-12 < 2^-11; the rounding adds 2^-8."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_05508_amd as P
+from gpu_util import launched
+from test_gpu_worker import U, out_like, untouched
+
+pytestmark = pytest.mark.gpu
+E4M3 = torch.float8_e4m3fn
+ACT = {"none": P.MLMC_ACT_NONE, "relu": P.MLMC_ACT_RELU, "gelu": P.MLMC_ACT_GELU}
+SIZES = [  # rows, outputs, inputs, pad, shift
+    (1, 1, 1, 0, 0), (1, 3, 5, 1, 1), (2, 17, 15, 0, 0), (3, 16, 16, 0, 0), (5, 33, 64, 0, 0), (1, 128, 257, 0, 0), (16, 100, 1000, 8, 0), (16, 4096, 4096, 0, 0), (1, 4096, 4096, 0, 0),
+    (17, 64, 128, 0, 0), (33, 65, 127, 1, 3), (40, 129, 130, 0, 0), (64, 128, 512, 0, 0), (100, 200, 300, 5, 0), (129, 257, 1023, 0, 0), (255, 256, 1024, 16, 16), (256, 512, 8192, 0, 0),
+    (300, 1000, 13, 0, 0), (513, 1025, 2049, 0, 0), (1000, 640, 4096, 0, 4), (2048, 2048, 1024, 0, 0), (2049, 2305, 1025, 3, 1), (4096, 4096, 512, 0, 0), (4100, 4000, 640, 0, 0), (37, 8192, 96, 0, 0),
+]
+
+
+def eight(t, pad=0, shift=0):
+    """A matrix in 8 bits, cut out of a larger buffer of NaN."""
+    n, d = t.shape
+    buf = torch.full((n * (d + pad) + shift,), 127, dtype=torch.uint8, device="cuda")
+    q = torch.as_strided(buf, (n, d), (d + pad, 1), shift).view(E4M3)
+    q.copy_(t.to(E4M3))
+    return q
+
+
+def whole(gen, n, d, pad=0, shift=0):
+    return eight(torch.randint(-3, 4, (n, d), device="cuda", generator=gen).float(), pad, shift)
+
+
+def powers(gen, n):
+    return torch.exp2(torch.randint(-3, 4, (n,), device="cuda", generator=gen).float())
+
+
+@pytest.mark.parametrize("n,m,k,pad,shift", SIZES)
+def test_linear_q8_to_the_bit(n, m, k, pad, shift):
+    print(f"linear_q8 n={n} m={m} k={k} pad={pad} shift={shift}", flush=True)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n * 7 + m * 3 + k)
+    x, w = whole(gen, n, k, pad, shift), whole(gen, m, k, 0 if k % 2 else pad, shift)
+    xs, ws = powers(gen, n), powers(gen, m)
+    bias = torch.randint(-8, 9, (m,), device="cuda", generator=gen).float()
+    residual = torch.randint(-8, 9, (n, m), device="cuda", generator=gen).to(torch.bfloat16)
+    v = (x.to(torch.float64) @ w.to(torch.float64).t().contiguous()) * xs.double()[:, None] * ws.double()
+    for act, r in (("none", None), ("relu", residual)):
+        y, buf = out_like(n, m, "bf16", pad, shift)
+        assert P.mlmc_linear_q8(x, xs, w, ws, bias, act=ACT[act], residual=r, y=y) is y
+        z = v + bias.double()
+        want = z if act == "none" else z.clamp(min=0) + r.double()
+        assert torch.equal(y, want.float().to(torch.bfloat16)), float((y.double() - want).abs().max())
+        untouched(buf, y)
+        if r is not None:      # in the place of the residual
+            P.mlmc_linear_q8(x, xs, w, ws, bias, act=ACT[act], residual=r, y=r)
+            assert torch.equal(r, y)
+    assert torch.equal(P.mlmc_linear_q8(x, xs, w, ws), v.float().to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("n,m,k", [(1, 4096, 4096), (300, 500, 2001), (2048, 2048, 2048), (128, 128, 8192), (4096, 4096, 4096)])
+def test_linear_q8_of_normal_entries(n, m, k, act):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n + m + k)
+    x, xs = P.mlmc_quantize(torch.empty((n, k), device="cuda").normal_(generator=gen))
+    w, ws = P.mlmc_quantize(torch.empty((m, k), device="cuda").normal_(0.0, k ** -0.5, generator=gen))
+    bias = torch.empty(m, device="cuda").normal_(generator=gen)
+    z = (x.to(torch.float64) * xs.double()[:, None]) @ (w.to(torch.float64) * ws.double()[:, None]).t().contiguous()
+    cut = 2.0 ** -11 * z.norm()
+    z = z + bias.double()
+    want = z if act == "none" else z.clamp(min=0) if act == "relu" else 0.5 * z * torch.erfc(-z / 2 ** 0.5)
+    y = P.mlmc_linear_q8(x, xs, w, ws, bias, act=ACT[act])
+    # slopes are at most 1.13 (gelu); gelu's tail for 16 bits is off by 1e-7, and fp32 sums and epilogue by (k / 32 + 40) U, both under 2^-14 of the rows' size
+    assert float((y.double() - want).norm()) <= 1.13 * float(cut) + (2.0 ** -8 + 2.0 ** -14) * float(want.norm()) + 2.0 ** -14 * float(z.norm())
+    assert torch.equal(P.mlmc_linear_q8(x, xs, w, ws, bias, act=ACT[act]), y)
+
+
+def test_linear_q8_scales():
+    """Scales of every size whose results bf16 has, zero and NaN ones among them; a NaN entry."""
+    x = eight(torch.ones((4, 64), device="cuda"))
+    w = eight(torch.ones((40, 64), device="cuda"))
+    xs = torch.tensor([2.0 ** -100, 2.0 ** 100, 0.0, float("nan")], device="cuda")
+    ws = torch.full((40,), 2.0 ** -20, device="cuda")
+    for more in (0, 30):      # few rows and tiles
+        xx, ss = eight(torch.ones((4 + more, 64), device="cuda")), torch.cat([xs, torch.ones(more, device="cuda")])
+        y = P.mlmc_linear_q8(xx, ss, w, ws)
+        assert bool((y[0] == 2.0 ** -114).all()) and bool((y[1] == 2.0 ** 86).all()) and bool((y[2] == 0).all()) and bool(y[3].isnan().all()) and bool((y[4:] == 2.0 ** -14).all())
+        xx[1, 3] = float("nan")
+        y = P.mlmc_linear_q8(xx, ss, w, ws)
+        assert bool(y[1].isnan().all()) and bool((y[0] == 2.0 ** -114).all())
+    assert x.shape == (4, 64)
+
+
+def test_linear_q8_kernels():
+    """The ways that the plan has: few rows, tiles, parts of the contraction, rows copied to aligned ones."""
+    def run(n, m, k, pad=0):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(1)
+        x, w = whole(gen, n, k, pad), whole(gen, m, k, pad)
+        return launched(lambda: P.mlmc_linear_q8(x, torch.ones(n, device="cuda"), w, torch.ones(m, device="cuda")))
+    assert run(1, 4096, 4096) == {"k_linear_q8_few"}
+    assert run(4096, 4096, 512) == {"k_linear_q8"}
+    assert "k_linear_join" in run(128, 128, 8192)
+    assert "k_linear_pack" in run(4096, 4096, 1024, pad=5)
+
+
+def test_linear_q8_without_rows():
+    w, s = eight(torch.ones((8, 16), device="cuda")), torch.ones(8, device="cuda")
+    assert P.mlmc_linear_q8(w[:0], s[:0], w, s).shape == (0, 8)
+    with pytest.raises(P.MlmcError):
+        P.mlmc_linear_q8(w.float(), s, w, s)
+    with pytest.raises(P.MlmcError):
+        P.mlmc_linear_q8(w, s, w, s[:7])
+    with pytest.raises(P.MlmcError):
+        P.mlmc_linear_q8(w, None, w, s)

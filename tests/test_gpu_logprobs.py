@@ -1,0 +1,240 @@
+"""Log probabilities of tokens, entropy, top alternatives and their gradient on the GPU against the definitions in 64 bits (oracle/worker.py).
+
+Tolerances are bounds, U = 2^-24.  With x_j = (s_j - m) / T: an argument of the exponential is off by 3 U |x_j| (difference, unit, product), the exponential by 2 U more, and no order used passes a
+term of the sum through more than 300 additions.  So log S is off by 302 U + 3 U E|x| + 2 U (E over p), a log probability by that and 4 U (|x| + |log p|).
+The entropy is log S - E x; E x is off by 3 U (E|x| + E x^2) + 305 U E|x| and, over S, by what S is off times E|x|."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_05508_amd as P
+from gpu_util import launched
+from oracle import worker as O
+from test_gpu_worker import U, UO, f64, near, out_like, rows, untouched
+
+pytestmark = pytest.mark.gpu
+INF, NAN = math.inf, math.nan
+SIZES = [  # rows, vocabulary, pad, shift, given, top
+    (1, 1, 0, 0, 1, 1), (3, 2, 1, 1, 2, 5), (2, 7, 0, 0, 1, 3), (5, 64, 0, 0, 1, 0), (4, 129, 3, 1, 0, 7), (33, 1000, 0, 0, 1, 20), (9, 1023, 1, 3, 7, 128), (600, 257, 0, 0, 1, 5),
+    (600, 5000, 0, 0, 1, 64), (3, 8191, 2, 0, 4, 64), (520, 8200, 0, 0, 1, 20), (2, 32768, 0, 0, 1, 128), (2, 50021, 3, 2, 1, 20), (1, 131072, 0, 0, 128, 128), (515, 33000, 0, 0, 1, 10),
+    (2, 262147, 0, 1, 1, 64), (513, 66000, 0, 0, 1, 64),
+]
+
+
+def forward_bounds(s, temperature, log_p):
+    with np.errstate(invalid="ignore", divide="ignore"):
+        x = np.abs((s - s.max(1, keepdims=True)) / temperature)
+        p = np.exp(log_p)
+        ex = np.where(p > 0, p * x, 0.0).sum(1)
+        exx = np.where(p > 0, p * x * x, 0.0).sum(1)
+    log_s = 304 * U + 3 * U * ex
+    h = log_s * (1 + ex) + U * (3 * (ex + exx) + 305 * ex) + 4 * U * (1 + ex)
+    return 1.01 * log_s, 1.01 * h, x
+
+
+def make(n, v, pad, shift, given, dtype, temperature, seed):
+    rng = np.random.default_rng(seed)
+    logits, s = rows(rng, n, v, dtype, pad, shift, std=2.5)
+    tokens = rng.integers(-1, v, (n, given))
+    return rng, logits, s, tokens
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v,pad,shift,given,top", SIZES)
+def test_token_logprobs(n, v, pad, shift, given, top, dtype):
+    print(f"token_logprobs n={n} v={v} pad={pad} shift={shift} given={given} top={top} {dtype}", flush=True)
+    temperature = 1.0 if v % 2 else 1.7
+    rng, logits, s, tokens = make(n, v, pad, shift, given, dtype, temperature, n * 7919 + v)
+    want, h, idx, val, stats = O.token_logprobs(s, tokens, top, temperature)
+    u = (s - s.max(1, keepdims=True)) / temperature
+    log_p = u - np.log(np.exp(u).sum(1, keepdims=True))
+    t_s, t_h, x = forward_bounds(s, temperature, log_p)
+    status = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    got = P.mlmc_token_logprobs(logits, torch.from_numpy(tokens).int().cuda() if given else None, top=top, temperature=temperature, with_entropy=True, with_stats=True, dev_status=status)
+    assert int(status) == 0
+    if given:
+        at = np.take_along_axis(log_p, np.maximum(tokens, 0), 1)
+        near("logprob", got.logprob, want, np.where(tokens < 0, 0.0, t_s[:, None] + 8 * U * np.abs(at)))
+    near("entropy", got.entropy, h, t_h + U * np.abs(h))
+    near("log of the sum", got.stats[:, 1], stats[:, 1], t_s + U * np.abs(stats[:, 1]))
+    assert np.array_equal(f64(got.stats[:, 0]), stats[:, 0])
+    if top:
+        assert np.array_equal(got.top_idx.cpu().numpy(), idx)
+        some = idx >= 0
+        assert (f64(got.top_logprob)[~some] == -INF).all()
+        near("top", got.top_logprob, val, np.where(some, t_s[:, None] + 8 * U * np.abs(np.where(some, val, 0.0)), 0.0)) if some.all() else None
+    bare = P.mlmc_token_logprobs(logits, top=top, temperature=temperature)
+    assert bare.logprob is None and bare.entropy is None and bare.stats is None
+    if top:
+        assert torch.equal(bare.top_idx, got.top_idx) and torch.equal(bare.top_logprob, got.top_logprob)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(600, 700), (600, 9000), (3, 9000), (2, 70001), (515, 33000), (513, 66000)])
+def test_ties_orders_and_masks(n, v, dtype):
+    """Equal logits, rows in ascending and descending order, rows of which few entries are left, a lowest value as a mask: the alternatives are those of a stable sort."""
+    rng = np.random.default_rng(v)
+    s = rng.normal(0, 2, (n, v)).astype(np.float32)
+    kinds = 8
+    for i in range(n):
+        k = i % kinds if n > 3 else (i + v) % kinds
+        if k == 0:
+            s[i] = 0.5
+        elif k == 1:
+            s[i] = np.linspace(-5, 5, v)
+        elif k == 2:
+            s[i] = np.linspace(5, -5, v)
+        elif k == 3:
+            s[i, rng.permutation(v)[3:]] = -INF
+        elif k == 4:
+            s[i, rng.permutation(v)[5:]] = -3.3895314e38      # the lowest of bf16
+        elif k == 5:
+            s[i] = rng.integers(0, 3, v)
+        elif k == 6:
+            s[i] = np.where(np.arange(v) % 2, 0.0, -0.0)
+            s[i, v - 4:] = 1.0
+    logits = torch.from_numpy(s).to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype]).cuda()
+    for top in (1, 5, 128):
+        got = P.mlmc_token_logprobs(logits, top=top, with_entropy=True)
+        _, h, idx, val, _ = O.token_logprobs(f64(logits)[:64], np.zeros((min(n, 64), 0), int), top, 1.0)
+        m = len(idx)
+        assert np.array_equal(got.top_idx[:m].cpu().numpy(), idx), np.argwhere(got.top_idx[:m].cpu().numpy() != idx)[:5]
+        gone = idx < 0
+        assert (f64(got.top_logprob[:m])[gone] == -INF).all()
+        # a spread of at most 40 (or a probability of 0): 304 U + 3 U 40 + 8 U 40, and a log probability of the lowest value to its own rounding
+        assert (np.abs(f64(got.top_logprob[:m])[~gone] - val[~gone]) <= 1000 * U + 4 * U * np.abs(val[~gone])).all()
+        assert (np.abs(f64(got.entropy[:m]) - h) <= 1e4 * U).all()
+        for i in range(kinds):      # the rows after the first 64 repeat the kinds without randomness
+            if n > 64 and i in (0, 1, 2, 6):
+                assert torch.equal(got.top_idx[i], got.top_idx[i + 64 * ((n - 1 - i) // 64)])
+
+
+@pytest.mark.parametrize("v", [100, 9000, 140000])
+def test_special_rows(v):
+    """NaN, +Inf and rows of nothing but -Inf; tokens that are padding, outside, or barred."""
+    s = np.random.default_rng(v).normal(0, 1, (6, v)).astype(np.float32)
+    s[1, 7] = NAN
+    s[2, 7] = INF
+    s[3] = -INF
+    s[4] = -INF
+    s[4, 5] = 3.0
+    tokens = np.array([[7, -1, v], [7, -1, v], [7, -1, 0], [7, -5, 0], [5, 6, -1], [0, 1, 2]])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    logits, at = torch.from_numpy(s).cuda(), torch.from_numpy(tokens).int().cuda()
+    got = P.mlmc_token_logprobs(logits, at, top=4, with_entropy=True, with_stats=True, dev_status=status)
+    assert int(status) == P.MLMC_DEV_RANGE
+    lp, h, idx, val = f64(got.logprob), f64(got.entropy), got.top_idx.cpu().numpy(), f64(got.top_logprob)
+    want, wh, widx, wval, _ = O.token_logprobs(s.astype(np.float64), tokens, 4, 1.0)
+    assert np.array_equal(np.isnan(lp), np.isnan(want)) and np.array_equal(np.isnan(h), np.isnan(wh)) and np.array_equal(idx, widx) and np.array_equal(np.isnan(val), np.isnan(wval))
+    assert lp[4, 0] == 0 and lp[4, 1] == -INF and h[4] == 0 and list(idx[4]) == [5, -1, -1, -1] and val[4, 0] == 0
+    P.mlmc_token_logprobs(logits[5:], at[5:], dev_status=status)
+    assert int(status) == 0
+    g = torch.ones((6, 3), device="cuda")
+    g[3] = 0.0
+    d = f64(P.mlmc_token_logprobs_backward(logits, got.stats, at, g))
+    assert np.isnan(d[1]).all() and np.isnan(d[2]).all() and (d[3] == 0).all() and np.isfinite(d[0]).all()
+    assert np.array_equal(d[4], np.where(np.arange(v) == 6, 1.0, np.where(np.arange(v) == 5, -1.0, 0.0)))      # two tokens: the one that is certain, and one that is barred
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v,pad,shift,given,top", SIZES)
+def test_token_logprobs_backward(n, v, pad, shift, given, top, dtype):
+    print(f"token_logprobs_backward n={n} v={v} pad={pad} shift={shift} given={given} top={top} {dtype}", flush=True)
+    if n * v > 5000000:
+        n = 40
+    temperature = 1.0 if v % 2 else 1.7
+    rng, logits, s, tokens = make(n, v, pad, shift, given, dtype, temperature, n + v)
+    if given > 1:
+        tokens[:, 1] = tokens[:, 0]      # the same token twice
+    at = torch.from_numpy(tokens).int().cuda() if given else None
+    got = P.mlmc_token_logprobs(logits, at, top=top, temperature=temperature, with_stats=True)
+    g, a, h = rng.normal(0, 1, (n, given)).astype(np.float32), rng.normal(0, 1, (n, top)).astype(np.float32), rng.normal(0, 1, n).astype(np.float32)
+    g[0] = 0.0
+    a[0] = 0.0
+    h[0] = 0.0
+    idx = got.top_idx.cpu().numpy() if top else None
+    u = (s - s.max(1, keepdims=True)) / temperature
+    log_p = u - np.log(np.exp(u).sum(1, keepdims=True))
+    p = np.exp(log_p)
+    t_s, t_h, x = forward_bounds(s, temperature, log_p)
+    entropy = -(p * log_p).sum(1, keepdims=True)
+    for with_h in (False, True):
+        hh = h if with_h else None
+        want = O.token_logprobs_backward(s, tokens if given else None, g, idx, a, hh, temperature)
+        dx, buf = out_like(n, v, dtype, pad, shift)
+        cuda = lambda t: torch.from_numpy(t).cuda()  # noqa: E731
+        kw = dict(top_idx=got.top_idx, dtop=cuda(a) if top else None, dentropy=cuda(h) if with_h else None, temperature=temperature)
+        P.mlmc_token_logprobs_backward(logits, got.stats, at, cuda(g) if given else None, dlogits=dx, **kw)
+        untouched(buf, dx)
+        weights = np.concatenate([np.where((tokens >= 0) & (tokens < v), np.abs(g), 0.0), np.where(idx >= 0, np.abs(a), 0.0) if top else np.zeros((n, 0))], 1).sum(1, keepdims=True)
+        hm = np.abs(h)[:, None] if with_h else 0.0
+        rel = t_s[:, None] + U * (3 * x + 8)                         # of p
+        tol = p * (weights * (rel + 270 * U) + hm * (np.abs(log_p + entropy) * (rel + 6 * U) + t_s[:, None] + t_h[:, None] + U * (4 * x + np.abs(entropy) + 8)))
+        hit = np.zeros((n, v))
+        for k, w in ((tokens, g), (idx, a)):
+            if k is not None:
+                for i in range(n):
+                    for t, q in zip(k[i], w[i]):
+                        if 0 <= t < v:
+                            hit[i, t] += abs(q)
+        tol = 1.01 * (tol + 258 * U * hit + 3 * U * np.abs(want) * temperature) / temperature
+        near("dlogits", dx, want, tol + UO[dtype] * (np.abs(want) + tol))
+        assert bool((dx[0] == 0).all())
+        inplace = logits.clone()
+        P.mlmc_token_logprobs_backward(inplace, got.stats, at, cuda(g) if given else None, dlogits=inplace, **kw)
+        assert torch.equal(inplace, dx)
+
+
+def test_gradient_against_differences():
+    """Central differences of the call's own results: their rounding is 600 U of magnitudes up to 20, over 2 h.  The alternatives are asked for as tokens: a step may change which they are."""
+    rng = np.random.default_rng(4)
+    s = torch.from_numpy(rng.normal(0, 2, (3, 40)).astype(np.float32)).cuda()
+    tokens = torch.tensor([[3, 9], [0, -1], [39, 39]], dtype=torch.int32, device="cuda")
+    g, a, e = (torch.from_numpy(rng.normal(0, 1, t).astype(np.float32)).cuda() for t in ((3, 2), (3, 4), (3,)))
+    r = P.mlmc_token_logprobs(s, tokens, top=4, temperature=1.5, with_stats=True)
+    d = P.mlmc_token_logprobs_backward(s, r.stats, tokens, g, r.top_idx, a, e, temperature=1.5)
+
+    def f(t):
+        q = P.mlmc_token_logprobs(t, torch.cat((tokens, r.top_idx), 1), temperature=1.5, with_entropy=True)
+        return (q.logprob.double() * torch.cat((g, a), 1)).sum(1) + q.entropy.double() * e
+    h = 2.0 ** -5
+    for j in range(40):
+        step = torch.zeros_like(s)
+        step[:, j] = h
+        up, down = s + step, s - step
+        slope = (f(up) - f(down)) / (up - down)[:, j].double()
+        assert bool(((slope - d[:, j].double()).abs() <= 2e-2 * h + 600 * U * 20 / h).all()), j
+
+
+def test_large_temperatures_and_logits():
+    s = torch.tensor([[1e30, -1e30, 0.0, 5.0], [-3e38, 3e38, 0.0, 1.0]], device="cuda")
+    r = P.mlmc_token_logprobs(s, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), top=2, temperature=1e35, with_entropy=True)
+    want = O.token_logprobs(f64(s), np.array([[0], [1]]), 2, 1e35)
+    assert r.logprob.shape == (2,)
+    assert np.allclose(f64(r.logprob), want[0][:, 0], rtol=1e-5, atol=1e-6) and np.allclose(f64(r.entropy), want[1], rtol=1e-5, atol=1e-6)
+    r = P.mlmc_token_logprobs(s, top=2, with_entropy=True)      # one entry has it all
+    assert bool((r.entropy == 0).all()) and r.top_idx.tolist() == [[0, 3], [1, 3]] and bool((r.top_logprob[:, 0] == 0).all())
+
+
+def test_rows_in_parts_and_whole_ones_take_their_own_kernels():
+    whole, parts = torch.zeros((600, 1000), device="cuda"), torch.zeros((2, 100000), device="cuda")
+    assert "k_logprobs_join" not in launched(lambda: P.mlmc_token_logprobs(whole, top=3))
+    assert "k_logprobs_join" in launched(lambda: P.mlmc_token_logprobs(parts, top=3))
+    assert launched(lambda: P.mlmc_token_logprobs_backward(parts, torch.zeros((2, 3), device="cuda"))) == {"k_logprobs_backward"}
+
+
+def test_as_a_teacher_of_the_distillation_loss():
+    """The alternatives' log probabilities are as good as their logits."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    teacher, student = (torch.empty((50, 3000), device="cuda").normal_(0.0, 2.0, generator=gen) for _ in range(2))
+    r = P.mlmc_token_logprobs(teacher, top=16)
+    val, idx = torch.topk(teacher, 16, dim=1)
+    assert torch.equal(idx.int(), r.top_idx)
+    for temperature in (1.0, 2.0):
+        a, da = P.mlmc_distill(student, r.top_idx, r.top_logprob, temperature)
+        b, db = P.mlmc_distill(student, idx.int(), val, temperature)
+        # log probabilities of up to 20 with 400 U of error each, times T^2 q (log q - log p) of up to 100 in all
+        assert float((a - b).abs().max()) <= 400 * U * 20 * 4 * 100 and float((da - db).abs().max()) <= 400 * U * 20 * 4
