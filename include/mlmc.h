@@ -430,7 +430,7 @@ mlmc_status mlmc_dropout(const void *x, int64_t ldx, int64_t rows, int64_t d, in
 
 /*
  * Log probabilities of given tokens, entropy and the top alternatives of every row of logits; with T = temperature log p_j = s_j / T - log sum exp(s_j' / T).
- *   logits: dev [rows][ldl], vocab <= 2^21;  tokens: dev [rows][given], 0 <= given <= MLMC_MAX_ANSWERS: a token below 0 is padding, its log probability is 0; one >= vocab
+ *   logits: dev [rows][ldl], vocab <= 2^20;  tokens: dev [rows][given], 0 <= given <= MLMC_MAX_ANSWERS: a token below 0 is padding, its log probability is 0; one >= vocab
  *   makes it NaN and sets MLMC_DEV_RANGE;  logprob: dev [rows][given] fp32 (out);  entropy: dev [rows] fp32 (out) or NULL: -sum p_j log p_j;
  *   top_idx, top_logprob: dev [rows][top] (out), 0 <= top <= MLMC_MAX_ANSWERS: the entries of the greatest logits in descending order, of equal ones the lowest index first, and their log
  *   probabilities.  A logit of -Inf has p = 0 and is no alternative: places without one have index -1 and -Inf.  With T = 1 these are a teacher's entries for mlmc_distill, at any

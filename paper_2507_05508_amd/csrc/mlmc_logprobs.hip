@@ -6,16 +6,16 @@
 //   d/ds_j of sum_k g_k log p_{i_k} + h H:   ( sum of the g_k with i_k = j  -  p_j sum_k g_k  -  h p_j (log p_j + H) ) / T
 // The alternatives are in order of (logit, lowest index first).
 //
-// The top K without a sort of the row: the row's threads form 256 groups, whose greatest entries are known from the maximum.  The K-th greatest of those is a bound that K entries reach, and
-// few more do (of 131072 independent entries 73 for K = 64, 177 for K = 128: those of which the K-th lies in a group of its own).  They are gathered in LDS and each counts how many are
-// before it.  Where ties or an order of the row bring more than the room for them, two bisections find the K-th greatest value and the index where its equals run out.
-//
-// Bound by memory: the logits are read once.
+// Bound by memory: the logits are read once.  One launch of waves without barriers, each with a stretch of a row in its registers, leaves the stretch's maximum and sums and the greatest entry
+// of every group of neighbouring entries; a wave a row then joins the sums and has the top K without a look at the whole row: K groups reach the K-th greatest of the groups' greatest entries, so
+// that no entry below it is among the top K, and none of the groups that do not reach it holds one.  Those K groups are read again, of 1024 groups at most; a few more than K of their entries
+// reach the bound (of 131072 independent entries 66 for K = 64), and each counts how many are before it.  Of equal entries the first K are enough; where an order of the row brings more than the
+// room for them (a row in ascending order), those found so far are cut to the top K by bisection.
 #include "mlmc_worker.h"
 
 namespace mlmc {
 
-constexpr int MOST_ANSWERS = MLMC_MAX_ANSWERS, ROOM = 1024, GROUPS = 256, PARTS_MAX = 32;
+constexpr int MOST_ANSWERS = MLMC_MAX_ANSWERS;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct LogprobArgs {
@@ -29,10 +29,10 @@ struct LogprobArgs {
     int32_t* top_idx;
     float *top_logprob, *stats;
     int32_t* dev_status;
-    int parts;                    // of a row, 1: a workgroup has the whole row and its answers
-    int64_t part_len;
-    float4* part_stats;           // [rows][parts] greatest entry, sum, sum of e log2 e
-    uint64_t* part_top;           // [rows][parts][top] keys in descending order, 0 behind the last
+    int stretches;                // of a row, a wave each
+    int groups, lanes;            // of a row, 0 without alternatives; lanes of a group, a power of two
+    float* stretch_stats;         // [rows][stretches][3] greatest entry, sum, sum of e log2 e
+    float* greatest;              // [rows][groups]
 };
 
 // Logits as numbers of the same order, -0 as 0.
@@ -46,7 +46,7 @@ __device__ inline uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
 __device__ inline float key_value(uint64_t key) { return unordered((uint32_t)(key >> 32)); }
 constexpr float LOWEST = -3.402823466e38f;
 
-// What a row (or all its parts) comes to.
+// What a row comes to.
 struct RowSums {
     float m, log_s, h;
     bool bad;
@@ -58,235 +58,378 @@ struct RowSums {
     __device__ float log_p(float v, float inv_temp) const { return (v - m) * inv_temp - log_s; }
 };
 
-template <int T> __device__ inline void write_given(const LogprobArgs& a, int64_t row, int32_t token, float logit, const RowSums& r) {
-    if ((int)threadIdx.x < a.given) {
-        const bool out = token >= a.vocab;
-        a.logprob[row * a.given + threadIdx.x] = token < 0 ? 0.f : out ? __builtin_nanf("") : r.log_p(logit, a.inv_temp);
-        if (out && a.dev_status) atomicOr(a.dev_status, MLMC_DEV_RANGE);
-    }
-    if (threadIdx.x == 0) {
-        if (a.entropy) a.entropy[row] = r.h;
-        if (a.stats) {
-            a.stats[3 * row] = r.m;
-            a.stats[3 * row + 1] = r.log_s;
-            a.stats[3 * row + 2] = r.h;
-        }
-    }
-}
 // alternative i of the row; key 0: there is none
 __device__ inline void write_top(const LogprobArgs& a, int64_t row, int i, uint64_t key, const RowSums& r) {
     a.top_idx[row * a.top + i] = r.bad || !key ? -1 : (int32_t)key_index(key);
     a.top_logprob[row * a.top + i] = r.bad ? __builtin_nanf("") : key ? r.log_p(key_value(key), a.inv_temp) : -INFINITY;
 }
 
-// A row, or a part of one, in the registers of T threads, N chunks of 16 bytes each.
-template <int DT, int T, int N, bool TOP> __global__ __launch_bounds__(T, N <= 8 ? 8 : 4) void k_logprobs(LogprobArgs a) {
-    constexpr int E = DT == MLMC_BF16 ? 8 : 4, W = T / 64;
-    constexpr float none = -INFINITY;
-    __shared__ float part[3][W];
-    __shared__ __align__(16) float greatest[TOP ? GROUPS : 1];
-    __shared__ uint64_t found[TOP ? ROOM : 1], best[TOP ? MOST_ANSWERS : 1];
-    __shared__ float bound;
-    __shared__ int number, counts[W];
-    const int64_t row = a.row0 + blockIdx.y, first = (int64_t)blockIdx.x * a.part_len;
-    const int len = (int)min(a.part_len, a.vocab - first), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lane_col = threadIdx.x * E;
-    const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds + first;
+// ---- stretches --------------------------------------------------------------------------------------------------------------------------
+
+constexpr int STRETCH_N = 4, STRETCH_WG = 256;
+template <int DT> constexpr int STRETCH = 64 * STRETCH_N * ENTRIES<DT>;   // entries of a wave
+
+// A wave's stretch as floats, its maximum and sums.  As much arithmetic as memory: ten vector instructions an entry (the exponential counts four) take 70 us for 2048 x 131072, whose read takes 105.
+template <int DT> __global__ __launch_bounds__(STRETCH_WG, 8) void k_logprobs(LogprobArgs a) {
+    constexpr int E = ENTRIES<DT>, N = STRETCH_N;
+    const int at = blockIdx.x * (blockDim.x / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= a.stretches) return;
+    const int64_t row = a.row0 + blockIdx.y;
+    const int first = at * STRETCH<DT>, lane = threadIdx.x & 63, lane_col = lane * E, vocab = (int)a.vocab;
+    const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
     chunk_t v[N];
+    if (first + STRETCH<DT> <= vocab) {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-        if (n * T * E < len) v[n] = load_chunk<DT>(s, lane_col + n * T * E, len);
-    int32_t token = -1;
-    float logit = 0.f;
-    if (a.parts == 1 && (int)threadIdx.x < a.given) {
-        token = a.tokens[row * a.given + threadIdx.x];
-        if (token >= 0 && token < a.vocab) logit = to_f32(s[token]);
+        for (int n = 0; n < N; ++n) v[n] = *(const chunk_u*)(s + first + lane_col + n * 64 * E);
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = load_chunk<DT>(s, first + lane_col + n * 64 * E, vocab);
     }
-    float f[E], mine = none;
+    float f[N][E], g[N], m = -INFINITY;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        if (n * T * E >= len) continue;
-        chunk_floats<DT>(f, v[n]);
+        chunk_floats<DT>(f[n], v[n]);
+        g[n] = -INFINITY;   // a NaN among numbers is passed over, a chunk of nothing else has -Inf
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine = fmaxf(mine, f[e]);
+        for (int e = 0; e < E; ++e) g[n] = fmaxf(g[n], f[n][e]);
+        m = fmaxf(m, g[n]);
     }
-    if (TOP) {
-        float g = mine;
-        if (T >= 512) g = fmaxf(g, dpp<0xB1, 0xF>(g, g));    // lanes 2k and 2k + 1
-        if (T >= 1024) g = fmaxf(g, dpp<0x4E, 0xF>(g, g));   // fours
-        if (threadIdx.x % (T / GROUPS) == 0) greatest[threadIdx.x / (T / GROUPS)] = g;
-        if (threadIdx.x == 0) number = 0;
-    }
-    float m = wave_max(mine);
-    if (lane == 0) part[0][wave] = m;
-    __syncthreads();
-#pragma unroll 4
-    for (int w = 0; w < W; ++w) m = fmaxf(m, part[0][w]);
-    const float from = m == none ? 0.f : m;
-    float sum = 0.f, elog = 0.f;
+    m = wave_max(m);
+    if (a.groups) {
+        const auto join = [&](auto other) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        if (n * T * E >= len) continue;
-        chunk_floats<DT>(f, v[n]);
+            for (int n = 0; n < N; ++n) g[n] = fmaxf(g[n], other(g[n]));
+        };
+        if (a.lanes >= 2) join([](float x) { return dpp<0xB1, 0xF>(x, x); });     // lanes 2k and 2k + 1
+        if (a.lanes >= 4) join([](float x) { return dpp<0x4E, 0xF>(x, x); });     // the pairs of four
+        if (a.lanes >= 8) join([](float x) { return dpp<0x141, 0xF>(x, x); });    // eight, mirrored
+        if (a.lanes >= 16) join([](float x) { return dpp<0x140, 0xF>(x, x); });   // sixteen
+        if (a.lanes >= 32) join([](float x) { return __shfl_xor(x, 16); });
+        if (a.lanes >= 64) join([](float x) { return __shfl_xor(x, 32); });
+        if ((lane & (a.lanes - 1)) == 0) {
+            const int shift = __builtin_ctz(a.lanes);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float t = (f[e] - from) * a.unit, x = __builtin_amdgcn_exp2f(t);
-            sum += x;
-            elog = fmaf(x, fmaxf(t, -1024.f), elog);   // x is 0 below that
+            for (int n = 0; n < N; ++n) {
+                const int chunk = (at * N + n) * 64 + lane;
+                if (chunk * E < vocab) a.greatest[row * a.groups + (chunk >> shift)] = g[n];
+            }
         }
+    }
+    const float from = m == -INFINITY ? 0.f : m, c = from * a.unit;
+    float sum = 0.f, elog = 0.f;
+    if (fabsf(c) < 65536.f) {
+        // (s - m) / T in one instruction.  What c was rounded by, at most 2^-8, scales all of them alike, and is taken out of the sums.
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float t = fmaf(f[n][e], a.unit, -c), x = __builtin_amdgcn_exp2f(t);
+                sum += x;
+                elog = fmaf(x, fmaxf(t, -1024.f), elog);   // x is 0 below that
+            }
+        const float off = -fmaf(from, a.unit, -c), scale = __builtin_amdgcn_exp2f(off);
+        elog = scale * fmaf(sum, off, elog);
+        sum *= scale;
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float t = (f[n][e] - from) * a.unit, x = __builtin_amdgcn_exp2f(t);
+                sum += x;
+                elog = fmaf(x, fmaxf(t, -1024.f), elog);
+            }
     }
     sum = wave_sum(sum);
     elog = wave_sum(elog);
-    if (lane == 0) {
-        part[1][wave] = sum;
-        part[2][wave] = elog;
-    }
-    if (TOP && wave == 0) {   // the greatest number of 16 bits that `top` groups reach
-        const float4 g = ((const float4*)greatest)[lane];
-        const uint32_t k[4] = {ordered(g.x) >> 16, ordered(g.y) >> 16, ordered(g.z) >> 16, ordered(g.w) >> 16};
-        uint32_t at = 0;
-#pragma unroll 1
-        for (int b = 15; b >= 0; --b) {
-            const uint32_t c = at | 1u << b;
-            int n = 0;
+    float* p = a.stretch_stats + 3 * (row * a.stretches + at);
+    if (lane < 3) p[lane] = lane == 0 ? m : lane == 1 ? sum : elog;
+}
+
+// ---- rows ---------------------------------------------------------------------------------------------------------------------------------
+
+constexpr int ROWS_T = 256, BINS = 256;
+constexpr int ROOM = 1024, LIST = 512, BATCH = 4;   // keys found, groups listed; loads in flight
+
+// Lanes below this one that are in the mask.
+__device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+// Sums over the lanes up to this one.
+template <int CTRL, int ROWS> __device__ inline int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ inline int wave_prefix(int v) {
+    v = dpp_add<0x111, 0xF>(v);
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);
+    return dpp_add<0x143, 0xC>(v);
+}
+// What the wave has written to LDS is there for all its lanes.
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The top keys among n of them (n > top), into the front of `found`, in any order; the least of them is returned.  One wave.
+__device__ inline uint64_t cut_to_top(uint64_t* found, int n, int top) {
+    constexpr int J = ROOM / 64;
+    const int lane = threadIdx.x;
+    uint64_t key[J];
+    wave_sync();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(k[i] >= c));
-            if (n >= a.top) at = c;
+    for (int j = 0; j < J; ++j) key[j] = j * 64 + lane < n ? found[j * 64 + lane] : 0;
+    uint64_t least = 0;
+    for (int b = 63; b >= 0; --b) {
+        const uint64_t c = least | 1ull << b;
+        int reach = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) reach += __popcll(__ballot(key[j] >= c));
+        if (reach >= top) least = c;
+        if (reach == top) break;
+    }
+    wave_sync();
+    int at = 0;
+    uint64_t smallest = ~0ull;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const bool keep = key[j] >= least;   // no two keys are equal: exactly `top`
+        const uint64_t mask = __ballot(keep);
+        if (keep) {
+            found[at + lanes_before(mask)] = key[j];
+            smallest = key[j] < smallest ? key[j] : smallest;
         }
-        if (lane == 0) bound = at <= ordered(none) >> 16 ? LOWEST : unordered(at << 16);   // never -Inf: that is no alternative
+        at += __popcll(mask);
+    }
+    wave_sync();
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)smallest, o);
+        smallest = other < smallest ? other : smallest;
+    }
+    return smallest;
+}
+
+// The top keys of a row by one wave, whatever ties and order it has, into the front of `found`: their number is returned.
+template <int DT> __device__ inline int top_by_bisection(const LogprobArgs& a, const entry_t<DT>* s, const float* g, uint64_t* found, uint32_t* list) {
+    constexpr int E = ENTRIES<DT>;
+    const int lane = threadIdx.x;
+    const auto group = [&](int r) { return r + lane < a.groups ? ordered(g[r + lane]) : 0u; };
+    // the greatest number that `top` groups reach; below that of the lowest logit there is no alternative
+    uint32_t bound = 0;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t c = bound | 1u << b;
+        int reach = 0;
+        for (int r = 0; r < a.groups; r += 64) reach += __popcll(__ballot(group(r) >= c));
+        if (reach >= a.top) bound = c;
+        if (reach == a.top) break;
+    }
+    bound = max(bound, ordered(LOWEST));
+    // the groups, in order: all that are above the bound, of those that reach it the first `top`
+    int listed = 0, ties = 0;
+    for (int r = 0; r < a.groups; r += 64) {
+        const uint32_t k = group(r);
+        const bool tie = k == bound;
+        const uint64_t tied = __ballot(tie);
+        const bool take = k > bound || (tie && ties + lanes_before(tied) < a.top);
+        const uint64_t mask = __ballot(take);
+        const int at = listed + lanes_before(mask);
+        if (take && at < 2 * MOST_ANSWERS) list[at] = r + lane;
+        listed += __popcll(mask);
+        ties += __popcll(tied);
+    }
+    listed = min(listed, 2 * MOST_ANSWERS);   // (never more)
+    wave_sync();
+    // their entries that reach the bound, 64 / lanes groups at a time
+    float b = unordered(bound);
+    bool equals = true;   // whether entries equal to b are still taken
+    int n = 0, equal = 0;
+    const int each = 64 / a.lanes, mine = lane / a.lanes, place = lane & (a.lanes - 1);
+    for (int i = 0; i < listed; i += each) {
+        const int at = i + mine;
+        const unsigned col = at < listed ? (list[at] * a.lanes + place) * E : (unsigned)a.vocab;
+        float f[E];
+        chunk_floats<DT>(f, load_chunk<DT>(s, col, a.vocab));   // -Inf past the row's end
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const bool hit = f[e] > b || (equals && f[e] == b);
+            const uint64_t mask = __ballot(hit);
+            if (hit) found[n + lanes_before(mask)] = key_of(f[e], col + e);
+            n += __popcll(mask);
+            equal += __popcll(__ballot(f[e] == b));
+        }
+        if (equal >= a.top) equals = false;   // what follows has higher indices
+        if (n > ROOM - 64 * E) {   // the next load may bring 64 * E
+            static_assert(ROOM - 64 * E >= MOST_ANSWERS, "there are more than `top`");
+            b = key_value(cut_to_top(found, n, a.top));
+            n = a.top;
+            equals = false;   // what follows and is equal to the last of them comes behind it
+        }
+    }
+    if (n > a.top) {
+        cut_to_top(found, n, a.top);
+        n = a.top;
+    }
+    return n;
+}
+
+// A row by a workgroup.  The bound by a histogram of the groups' greatest entries over their range (its end 64 temperatures below the greatest): the bin in which the K-th lies, then the least
+// group in it or above.  Rows that have too many groups there, as with ties, go to one wave.  R: groups of a thread, 0 without alternatives.
+template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_rows(LogprobArgs a) {
+    constexpr int E = ENTRIES<DT>, W = ROWS_T / 64;
+    __shared__ uint64_t found[R ? ROOM : 1];
+    __shared__ uint32_t list[R ? LIST : 1];
+    __shared__ int bins[R ? BINS : 1], totals[W];
+    __shared__ float lows[W];
+    __shared__ float total[3];
+    __shared__ int listed, number, edge;
+    __shared__ uint32_t bound;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t row = a.row0 + blockIdx.x;
+    const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
+    const float* groups = a.greatest + row * a.groups;
+    float g[R ? R : 1];
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) g[r] = r * ROWS_T + t < a.groups ? groups[r * ROWS_T + t] : -INFINITY;
+        bins[t] = 0;
+    }
+    int32_t token = -1;
+    float logit = 0.f;
+    if (t < a.given) {
+        token = a.tokens[row * a.given + t];
+        if (token >= 0 && token < a.vocab) logit = to_f32(s[token]);
+    }
+    const float* stretch = a.stretch_stats + 3 * row * a.stretches;
+    float m = -INFINITY;
+    if (R > 0 || wave == 0) {
+        for (int p = lane; p < a.stretches; p += 64) m = fmaxf(m, stretch[3 * p]);
+        m = wave_max(m);
+    }
+    if (wave == 0) {   // the stretches' sums: each lane's, one after the other, then the lanes'
+        float sum = 0.f, elog = 0.f;
+        for (int p = lane; p < a.stretches; p += 64) {
+            const float from = stretch[3 * p], part = stretch[3 * p + 1];
+            const float x = from == -INFINITY ? -1024.f : fmaxf((from - m) * a.unit, -1024.f), w = __builtin_amdgcn_exp2f(x);
+            sum = fmaf(part, w, sum);
+            elog = fmaf(w, fmaf(part, x, stretch[3 * p + 2]), elog);
+        }
+        sum = wave_sum(sum);
+        elog = wave_sum(elog);
+        if (lane == 0) {
+            total[0] = m;
+            total[1] = sum;
+            total[2] = elog;
+            listed = number = 0;
+            edge = -1;
+            bound = ~0u;
+        }
+    }
+    if constexpr (R > 0) {
+        float low = m;
+#pragma unroll
+        for (int r = 0; r < R; ++r) low = fminf(low, g[r] == -INFINITY ? m : g[r]);
+        low = -wave_max(-low);
+        if (lane == 0) lows[wave] = low;
     }
     __syncthreads();
-    sum = elog = 0.f;
-#pragma unroll 4
-    for (int w = 0; w < W; ++w) {
-        sum += part[1][w];
-        elog += part[2][w];
+    const RowSums sums(total[0], total[1], total[2]);
+    if (t < a.given) {
+        const bool out = token >= a.vocab;
+        a.logprob[row * a.given + t] = token < 0 ? 0.f : out ? __builtin_nanf("") : sums.log_p(logit, a.inv_temp);
+        if (out && a.dev_status) atomicOr(a.dev_status, MLMC_DEV_RANGE);
     }
-    int n_top = 0;
-    if constexpr (TOP) {
-        const float least = bound;
-        // entries that `take` has, into `found`, in any order
-        const auto gather = [&](auto take) {
+    if (t == 0 && a.entropy) a.entropy[row] = sums.h;
+    if (a.stats && t < 3) a.stats[3 * row + t] = t == 0 ? sums.m : t == 1 ? sums.log_s : sums.h;
+    if constexpr (R > 0) {
+        if (sums.bad) {
+            for (int i = t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+            return;
+        }
+        float low = m;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if (n * T * E >= len) continue;
-                chunk_floats<DT>(f, v[n]);
+        for (int w = 0; w < W; ++w) low = fminf(low, lows[w]);
+        const float scale = (BINS - 0.5f) / fminf(m - low, 64.f / a.inv_temp);
+        int bin[R];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int col = lane_col + n * T * E + e;
-                    if (take(f[e], col)) {
-                        const int at = atomicAdd(&number, 1);
-                        if (at < ROOM) found[at] = key_of(f[e], (uint32_t)(first + col));
+        for (int r = 0; r < R; ++r) {   // not rising with g: a group in a lower bin is greater than one in a higher
+            bin[r] = g[r] == -INFINITY ? BINS : (int)fminf((m - g[r]) * scale, BINS - 1.f);   // (equal groups are all in the last one: fminf takes 0 times infinity for no number)
+            if (bin[r] < BINS) atomicAdd(&bins[bin[r]], 1);
+        }
+        __syncthreads();
+        const int own = bins[t], prefix = wave_prefix(own);
+        if (lane == 63) totals[wave] = prefix;
+        __syncthreads();
+        int upto = prefix, all = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) upto += totals[w];
+            all += totals[w];
+        }
+        if (upto >= a.top && upto - own < a.top) edge = upto <= LIST ? t : BINS;
+        if (t == 0 && all < a.top) {   // fewer groups than alternatives: all that are not -Inf, and all of their entries
+            edge = BINS - 1;
+            bound = ordered(LOWEST);
+        }
+        __syncthreads();
+        int n;
+        const int last = edge;
+        if (last < BINS) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (bin[r] <= last) {
+                    list[atomicAdd(&listed, 1)] = r * ROWS_T + t;
+                    atomicMin(&bound, ordered(g[r]));
+                }
+            __syncthreads();
+            const int many = listed;
+            const float least = unordered(bound);
+            const int each = 64 / a.lanes, mine = lane / a.lanes, place = lane & (a.lanes - 1);
+            for (int i = wave * each; i < many; i += W * each * BATCH) {
+                chunk_t v[BATCH];
+                unsigned col[BATCH];
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    const int at = i + u * W * each + mine;
+                    col[u] = at < many ? (list[at] * a.lanes + place) * E : (unsigned)a.vocab;
+                    v[u] = load_chunk<DT>(s, col[u], a.vocab);   // -Inf past the row's end
+                }
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    float f[E];
+                    chunk_floats<DT>(f, v[u]);
+                    int hits = 0;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) hits += f[e] >= least;
+                    if (hits) {
+                        int at = atomicAdd(&number, hits);
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (f[e] >= least) {
+                                if (at < ROOM) found[at] = key_of(f[e], col[u] + e);
+                                ++at;
+                            }
                     }
                 }
             }
-        };
-        if (mine >= least) gather([&](float x, int) { return x >= least; });
-        __syncthreads();
-        int n = number;
-        if (n > ROOM) {
-            // how many entries of the workgroup `take` has
-            const auto count = [&](auto take) {
-                int c = 0;
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    if (n * T * E >= len) continue;
-                    chunk_floats<DT>(f, v[n]);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) c += __popcll(__ballot(take(f[e], lane_col + n * T * E + e)));
-                }
-                __syncthreads();
-                if (lane == 0) counts[wave] = c;
-                __syncthreads();
-                c = 0;
-                for (int w = 0; w < W; ++w) c += counts[w];
-                return c;
-            };
-            uint32_t at = ordered(least), up = ordered(m);   // `top` entries reach at; the K-th greatest lies in [at, up]
-            while (at < up) {
-                const uint32_t mid = at + (up - at + 1) / 2;
-                if (count([&](float x, int) { return x >= unordered(mid); }) >= a.top) at = mid;
-                else up = mid - 1;
-            }
-            const float kth = unordered(at);
-            const int left = a.top - count([&](float x, int) { return x > kth; });
-            int lo = 0, hi = len - 1;   // the index up to which `left` entries are equal to it
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (count([&](float x, int col) { return x == kth && col <= mid; }) >= left) hi = mid;
-                else lo = mid + 1;
-            }
             __syncthreads();
-            if (threadIdx.x == 0) number = 0;
-            __syncthreads();
-            gather([&](float x, int col) { return x > kth || (x == kth && col <= lo); });
-            __syncthreads();
-            n = number;   // `top` of them
+            n = number;
         }
-        for (int i = threadIdx.x; i < n; i += T) {
+        if (last == BINS || n > ROOM) {
+            if (wave == 0) {
+                n = top_by_bisection<DT>(a, s, groups, found, list);
+                if (lane == 0) number = n;
+            }
+            __syncthreads();
+            n = number;
+        }
+        for (int i = t; i < n; i += ROWS_T) {
             const uint64_t key = found[i];
             int before = 0;
 #pragma unroll 8
             for (int o = 0; o < n; ++o) before += found[o] > key;
-            if (before < a.top) best[before] = key;
+            if (before < a.top) write_top(a, row, before, key, sums);
         }
-        __syncthreads();
-        n_top = min(n, a.top);
+        for (int i = n + t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
     }
-    if (a.parts > 1) {
-        const int64_t at = row * a.parts + blockIdx.x;
-        if (threadIdx.x == 0) a.part_stats[at] = make_float4(m, sum, elog, 0.f);
-        if constexpr (TOP)
-            for (int i = threadIdx.x; i < a.top; i += T) a.part_top[at * a.top + i] = i < n_top ? best[i] : 0;
-        return;
-    }
-    const RowSums r(m, sum, elog);
-    write_given<T>(a, row, token, logit, r);
-    if constexpr (TOP)
-        for (int i = threadIdx.x; i < a.top; i += T) write_top(a, row, i, i < n_top ? best[i] : 0, r);
-}
-
-// The parts of a row: their sums scaled to the greatest maximum, in their order, and their lists, each of which says by bisection how many of its entries are before one of another.
-constexpr int JOIN_T = 256;
-__global__ __launch_bounds__(JOIN_T) void k_logprobs_join(LogprobArgs a, int dtype) {
-    extern __shared__ uint64_t list[];   // [parts][top]
-    __shared__ int number;
-    const int64_t row = a.row0 + blockIdx.x;
-    const int lane = threadIdx.x & 63, all = a.parts * a.top;
-    int32_t token = -1;
-    float logit = 0.f;
-    if ((int)threadIdx.x < a.given) {
-        token = a.tokens[row * a.given + threadIdx.x];
-        if (token >= 0 && token < a.vocab) logit = dtype == MLMC_F32 ? ((const float*)a.s)[row * a.lds + token] : to_f32(((const __bf16*)a.s)[row * a.lds + token]);
-    }
-    const float4 p = lane < a.parts ? a.part_stats[row * a.parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-    if (threadIdx.x == 0) number = 0;
-    const uint64_t* from = a.part_top + row * all;
-    for (int i = threadIdx.x; i < all; i += JOIN_T) list[i] = from[i];
-    const float m = wave_max(p.x), t = p.x == -INFINITY ? -1024.f : fmaxf((p.x - m) * a.unit, -1024.f), w = __builtin_amdgcn_exp2f(t);
-    const RowSums r(m, wave_sum(p.y * w), wave_sum(w * fmaf(p.y, t, p.z)));
-    write_given<JOIN_T>(a, row, token, logit, r);
-    if (a.top == 0) return;
-    __syncthreads();
-    for (int i = threadIdx.x; i < all; i += JOIN_T) {
-        const uint64_t key = list[i];
-        if (!key) continue;
-        atomicAdd(&number, 1);
-        const int own = i / a.top;
-        int before = i - own * a.top;
-        for (int q = 0; q < a.parts && before < a.top; ++q) {
-            if (q == own) continue;
-            int lo = 0, hi = a.top;   // entries of list q that are greater
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (list[q * a.top + mid] > key) lo = mid + 1;
-                else hi = mid;
-            }
-            before += lo;
-        }
-        if (before < a.top) write_top(a, row, before, key, r);
-    }
-    __syncthreads();
-    for (int i = number + threadIdx.x; i < a.top; i += JOIN_T) write_top(a, row, i, 0, r);
 }
 
 // ---- the gradient ---------------------------------------------------------------------------------------------------------------------
@@ -395,44 +538,33 @@ template <int DT> __global__ __launch_bounds__(GRAD_T, 8) void k_logprobs_backwa
 
 // ---- plans ----------------------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t VOCAB_MAX = (int64_t)1 << 21;
-// A row by one workgroup, or in parts: where rows are too few for the CUs, and where a row does not fit in a workgroup's registers.
-struct LogprobPlan { int parts; int64_t part_len; };
-static LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int dtype) {
-    const int64_t fit = dtype == MLMC_BF16 ? 65536 : 32768, least = 4096;
-    int64_t parts = (vocab + fit - 1) / fit;
-    const int64_t want = rows ? (512 + rows - 1) / rows : 1, most = (vocab + least - 1) / least;
-    const int64_t fill = want < most ? want : most;
-    parts = parts > fill ? parts : fill;
-    parts = parts < PARTS_MAX ? parts : PARTS_MAX;
-    const int64_t len = ((vocab + parts - 1) / parts + 7) / 8 * 8;
-    return {(int)((vocab + len - 1) / len), len};
+constexpr int64_t VOCAB_MAX = (int64_t)1 << 20;
+constexpr int GROUPS_MOST = 1024;   // more only of rows that have them with all lanes of a wave
+
+struct LogprobPlan { int stretches, groups, lanes; };
+static LogprobPlan logprob_plan(int64_t vocab, int dtype, int top) {
+    const int64_t E = dtype == MLMC_BF16 ? 8 : 4, stretch = 64 * STRETCH_N * E, chunks = (vocab + E - 1) / E;
+    LogprobPlan p = {(int)((vocab + stretch - 1) / stretch), 0, 1};
+    while (p.lanes < 64 && (chunks + p.lanes - 1) / p.lanes > GROUPS_MOST) p.lanes *= 2;
+    if (top) p.groups = (int)((chunks + p.lanes - 1) / p.lanes);
+    return p;
 }
-static size_t logprob_bytes(const LogprobPlan& p, int64_t rows, int top) {
-    return p.parts > 1 ? (size_t)rows * p.parts * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
-}
+static size_t logprob_bytes(const LogprobPlan& p, int64_t rows) { return (size_t)rows * ((size_t)p.stretches * 3 + p.groups) * sizeof(float); }
 static bool logprob_sizes_ok(int64_t rows, int64_t vocab, int given, int top) {
     return rows >= 0 && rows < ((int64_t)1 << 31) && vocab >= 1 && vocab <= VOCAB_MAX && given >= 0 && given <= MOST_ANSWERS && top >= 0 && top <= MOST_ANSWERS;
 }
 static bool temperature_ok(float t) { return t > 0.0f && t <= 3.402823e38f && 1.4426950408889634f / t <= 3.402823e38f; }
 constexpr int64_t ROW_SLICE = 32768;   // rows of a launch: they are the grid's second axis
 
-template <int DT, int T, int N> static mlmc_status logprob_launch(const LogprobArgs& a, dim3 grid, hipStream_t st) {
-    if (a.top) MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs<DT, T, N, true><<<grid, T, 0, st>>>(a)));
-    else MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs<DT, T, N, false><<<grid, T, 0, st>>>(a)));
-    return MLMC_OK;
-}
 template <int DT> static mlmc_status logprob_run(LogprobArgs a, hipStream_t st) {
-    constexpr int64_t E = DT == MLMC_BF16 ? 8 : 4;
+    const int each = a.stretches < STRETCH_WG / 64 ? a.stretches : STRETCH_WG / 64;
     for (; a.row0 < a.rows; a.row0 += ROW_SLICE) {
         const unsigned rows = (unsigned)(a.rows - a.row0 < ROW_SLICE ? a.rows - a.row0 : ROW_SLICE);
-        const dim3 grid((unsigned)a.parts, rows);
-        const mlmc_status rc = a.part_len <= 256 * 4 * E   ? logprob_launch<DT, 256, 4>(a, grid, st)
-                               : a.part_len <= 512 * 8 * E  ? logprob_launch<DT, 512, 8>(a, grid, st)
-                               : a.part_len <= 1024 * 8 * E ? logprob_launch<DT, 1024, 8>(a, grid, st)
-                                                            : logprob_launch<DT, 1024, 16>(a, grid, st);
-        if (rc != MLMC_OK) return rc;
-        if (a.parts > 1) MLMC_LAUNCH(K_LOGPROBS_JOIN, st, (k_logprobs_join<<<rows, JOIN_T, (size_t)a.parts * a.top * sizeof(uint64_t), st>>>(a, DT)));
+        MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs<DT><<<dim3((unsigned)((a.stretches + each - 1) / each), rows), each * 64, 0, st>>>(a)));
+        if (a.groups == 0) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 0><<<rows, ROWS_T, 0, st>>>(a)));
+        else if (a.groups <= ROWS_T) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 1><<<rows, ROWS_T, 0, st>>>(a)));
+        else if (a.groups <= 4 * ROWS_T) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 4><<<rows, ROWS_T, 0, st>>>(a)));
+        else MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 16><<<rows, ROWS_T, 0, st>>>(a)));
     }
     return MLMC_OK;
 }
@@ -454,7 +586,7 @@ extern "C" {
 
 size_t mlmc_token_logprobs_workspace(int64_t rows, int64_t vocab, int top) {
     if (!logprob_sizes_ok(rows, vocab, 0, top) || rows == 0) return 0;
-    const size_t a = logprob_bytes(logprob_plan(rows, vocab, MLMC_F32), rows, top), b = logprob_bytes(logprob_plan(rows, vocab, MLMC_BF16), rows, top);
+    const size_t a = logprob_bytes(logprob_plan(vocab, MLMC_F32, top), rows), b = logprob_bytes(logprob_plan(vocab, MLMC_BF16, top), rows);
     return a > b ? a : b;
 }
 
@@ -469,15 +601,15 @@ mlmc_status mlmc_token_logprobs(const void* logits, int64_t ldl, int64_t rows, i
         if (given && (!tokens || !f32_ptr_ok(tokens) || !logprob || !f32_ptr_ok(logprob))) return MLMC_EINVAL;
         if (top && (!top_idx || !f32_ptr_ok(top_idx) || !top_logprob || !f32_ptr_ok(top_logprob))) return MLMC_EINVAL;
     }
-    const LogprobPlan p = logprob_plan(rows, vocab, dtype);
-    const size_t need = logprob_bytes(p, rows, top);
-    if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
+    const LogprobPlan p = logprob_plan(vocab, dtype, top);
+    const size_t need = logprob_bytes(p, rows);
+    if (rows > 0 && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     if (dev_status) MLMC_LAUNCH(K_ZERO, st, (k_logprobs_clear<<<1, 1, 0, st>>>(dev_status)));
     if (rows == 0) return MLMC_OK;
     LogprobArgs a = {};
     a.s = logits; a.lds = ldl; a.rows = rows; a.vocab = vocab; a.tokens = tokens; a.given = given; a.top = top; a.inv_temp = 1.0f / temperature;
     a.unit = LOG2E / temperature; a.logprob = logprob; a.entropy = entropy; a.top_idx = top_idx; a.top_logprob = top_logprob; a.stats = stats; a.dev_status = dev_status;
-    a.parts = p.parts; a.part_len = p.part_len; a.part_stats = (float4*)ws; a.part_top = (uint64_t*)((float4*)ws + rows * p.parts);
+    a.stretches = p.stretches; a.groups = p.groups; a.lanes = p.lanes; a.stretch_stats = (float*)ws; a.greatest = (float*)ws + rows * 3 * p.stretches;
     return dtype == MLMC_F32 ? logprob_run<MLMC_F32>(a, st) : logprob_run<MLMC_BF16>(a, st);
 }
 

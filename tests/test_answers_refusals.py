@@ -70,7 +70,7 @@ def logprobs_backward(**k):
     (dropout, dict(rows=-1)), (dropout, dict(d=0)), (dropout, dict(ldx=7)), (dropout, dict(ldy=7)), (dropout, dict(res=A, ldr=7)), (dropout, dict(p=-0.1)), (dropout, dict(p=1.0)),
     (dropout, dict(p=1 - 2.0 ** -17)), (dropout, dict(p=NAN)), (dropout, dict(step=1 << 32)), (dropout, dict(row0=-1)), (dropout, dict(row0=(1 << 32) - 1)), (dropout, dict(dtype=2)),
     (dropout, dict(row0=(1 << 63) - 1)), (dropout, dict(x=A + 1)), (dropout, dict(y=None)),
-    (logprobs, dict(v=0)), (logprobs, dict(v=(1 << 21) + 1, ldl=1 << 22)), (logprobs, dict(ldl=7)), (logprobs, dict(given=129)), (logprobs, dict(top=129)), (logprobs, dict(top=-1)),
+    (logprobs, dict(v=0)), (logprobs, dict(v=(1 << 20) + 1, ldl=1 << 22)), (logprobs, dict(ldl=7)), (logprobs, dict(given=129)), (logprobs, dict(top=129)), (logprobs, dict(top=-1)),
     (logprobs, dict(given=-1)), (logprobs, dict(temp=0.0)), (logprobs, dict(temp=INF)), (logprobs, dict(temp=1e-45)), (logprobs, dict(tok=None)), (logprobs, dict(lp=None)),
     (logprobs, dict(idx=None)), (logprobs, dict(val=A + 1)), (logprobs, dict(h=A + 2)), (logprobs, dict(stats=A + 1)), (logprobs, dict(st=A + 1)), (logprobs, dict(s=A + 2)),
     (logprobs, dict(v=131072, ldl=131072, ws=None)), (logprobs, dict(v=131072, ldl=131072, wsb=64)),
@@ -93,7 +93,7 @@ def test_no_rows_is_no_work():
 
 def test_workspace_of_refused_sizes_is_zero():
     for f, a in ((P.mlmc_rms_norm_workspace, (-1, 8)), (P.mlmc_rms_norm_workspace, (1, 0)), (P.mlmc_linear_q8_workspace, (1, 0, 1)), (P.mlmc_linear_q8_workspace, (-1, 1, 1)),
-                 (P.mlmc_token_logprobs_workspace, (1, 0, 1)), (P.mlmc_token_logprobs_workspace, (1, 8, 129)), (P.mlmc_token_logprobs_workspace, (1, (1 << 21) + 1, 1))):
+                 (P.mlmc_token_logprobs_workspace, (1, 0, 1)), (P.mlmc_token_logprobs_workspace, (1, 8, 129)), (P.mlmc_token_logprobs_workspace, (1, (1 << 20) + 1, 1))):
         assert f(*a) == 0
 
 

@@ -218,11 +218,10 @@ def test_large_temperatures_and_logits():
     assert bool((r.entropy == 0).all()) and r.top_idx.tolist() == [[0, 3], [1, 3]] and bool((r.top_logprob[:, 0] == 0).all())
 
 
-def test_rows_in_parts_and_whole_ones_take_their_own_kernels():
-    whole, parts = torch.zeros((600, 1000), device="cuda"), torch.zeros((2, 100000), device="cuda")
-    assert "k_logprobs_join" not in launched(lambda: P.mlmc_token_logprobs(whole, top=3))
-    assert "k_logprobs_join" in launched(lambda: P.mlmc_token_logprobs(parts, top=3))
-    assert launched(lambda: P.mlmc_token_logprobs_backward(parts, torch.zeros((2, 3), device="cuda"))) == {"k_logprobs_backward"}
+def test_kernels():
+    x = torch.zeros((600, 1000), device="cuda")
+    assert launched(lambda: P.mlmc_token_logprobs(x, top=3)) == {"k_logprobs", "k_logprobs_rows"}
+    assert launched(lambda: P.mlmc_token_logprobs_backward(x, torch.zeros((600, 3), device="cuda"))) == {"k_logprobs_backward"}
 
 
 def test_as_a_teacher_of_the_distillation_loss():
