@@ -148,8 +148,8 @@ template <int DT> __global__ __launch_bounds__(STRETCH_WG, 8) void k_logprobs(Lo
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------------------------
 
-constexpr int ROWS_T = 256, BINS = 256;
 constexpr int ROOM = 1024, LIST = 512, BATCH = 4;   // keys found, groups listed; loads in flight
+constexpr int SHORT_CHUNKS = 1024;                  // of a row that one workgroup has in its registers
 
 // Lanes below this one that are in the mask.
 __device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
@@ -271,17 +271,94 @@ template <int DT> __device__ inline int top_by_bisection(const LogprobArgs& a, c
     return n;
 }
 
-// A row by a workgroup.  The bound by a histogram of the groups' greatest entries over their range (its end 64 temperatures below the greatest): the bin in which the K-th lies, then the least
-// group in it or above.  Rows that have too many groups there, as with ties, go to one wave.  R: groups of a thread, 0 without alternatives.
+// The bound that the top K reach, by a histogram of the groups' greatest entries over their range, which ends 64 temperatures below the greatest: 256 bins, of which a lower one holds greater
+// entries.  `edge`: the bin in which the K-th lies (BINS: there are fewer), `upto`: the groups in it and above.  Each wave finds it by itself.
+constexpr int ROWS_T = 256, BINS = 256;
+struct Bound {
+    float m, scale;
+    int edge, upto;
+    __device__ Bound(float m_, float low, float inv_temp) : m(m_), scale((BINS - 0.5f) / fminf(m_ - low, 64.f / inv_temp)), edge(0), upto(0) {}
+    // (equal groups are all in the last one: fminf takes 0 times infinity for no number)
+    __device__ int bin(float g) const { return g == -INFINITY ? BINS : (int)fminf((m - g) * scale, BINS - 1.f); }
+    __device__ void count(int* bins, int b) const {
+        if (b < BINS) atomicAdd(&bins[b], 1);
+    }
+    __device__ void find(const int* bins, int top) {
+        const int lane = threadIdx.x & 63;
+        const int4 own = ((const int4*)bins)[lane];
+        const int four = own.x + own.y + own.z + own.w, behind = wave_prefix(four);
+        const uint64_t reach = __ballot(behind >= top);
+        edge = BINS;
+        upto = __builtin_amdgcn_readlane(behind, 63);
+        if (!reach) return;
+        const int at = __ffsll((unsigned long long)reach) - 1, each[4] = {own.x, own.y, own.z, own.w};
+        int e = 0, n = behind - four;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (n < top) {
+                n += each[k];
+                e = 4 * lane + k;
+            }
+        edge = __builtin_amdgcn_readlane(e, at);
+        upto = __builtin_amdgcn_readlane(n, at);
+    }
+    // a number that the groups up to the edge reach, a little below the bin's end for what its arithmetic is rounded by; never -Inf, which is no alternative
+    __device__ float least() const { return edge >= BINS - 1 ? LOWEST : fmaxf(m - (edge + 1.01f) / scale - fabsf(m) * 0x1p-22f, LOWEST); }
+};
+
+// Entries of a thread's chunk that reach `least`, into `found` as far as there is room.
+template <int E> __device__ inline void collect(const float (&f)[E], float least, unsigned col, uint64_t* found, int* number) {
+    int hits = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) hits += f[e] >= least;
+    if (!hits) return;
+    int at = atomicAdd(number, hits);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (f[e] >= least) {
+            if (at < ROOM) found[at] = key_of(f[e], col + e);
+            ++at;
+        }
+}
+// The n keys found, each at its place.
+__device__ inline void write_found(const LogprobArgs& a, int64_t row, const uint64_t* found, int n, const RowSums& sums) {
+    for (int i = threadIdx.x; i < n; i += ROWS_T) {
+        const uint64_t key = found[i];
+        int before = 0;
+#pragma unroll 8
+        for (int o = 0; o < n; ++o) before += found[o] > key;
+        if (before < a.top) write_top(a, row, before, key, sums);
+    }
+    for (int i = n + threadIdx.x; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+}
+__device__ inline void write_sums(const LogprobArgs& a, int64_t row, int32_t token, float logit, const RowSums& sums) {
+    const int t = threadIdx.x;
+    if (t < a.given) {
+        const bool out = token >= a.vocab;
+        a.logprob[row * a.given + t] = token < 0 ? 0.f : out ? __builtin_nanf("") : sums.log_p(logit, a.inv_temp);
+        if (out && a.dev_status) atomicOr(a.dev_status, MLMC_DEV_RANGE);
+    }
+    if (t == 0 && a.entropy) a.entropy[row] = sums.h;
+    if (a.stats && t < 3) a.stats[3 * row + t] = t == 0 ? sums.m : t == 1 ? sums.log_s : sums.h;
+}
+template <int DT> __device__ inline int32_t load_token(const LogprobArgs& a, int64_t row, float& logit) {
+    int32_t token = -1;
+    logit = 0.f;
+    if ((int)threadIdx.x < a.given) {
+        token = a.tokens[row * a.given + threadIdx.x];
+        if (token >= 0 && token < a.vocab) logit = to_f32(((const entry_t<DT>*)a.s)[row * a.lds + token]);
+    }
+    return token;
+}
+
+// A row of several stretches by a workgroup.  Rows that have too many groups or entries at the bound, as with ties, go to one wave.  R: groups of a thread, 0 without alternatives.
 template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_rows(LogprobArgs a) {
     constexpr int E = ENTRIES<DT>, W = ROWS_T / 64;
     __shared__ uint64_t found[R ? ROOM : 1];
     __shared__ uint32_t list[R ? LIST : 1];
-    __shared__ int bins[R ? BINS : 1], totals[W];
-    __shared__ float lows[W];
-    __shared__ float total[3];
-    __shared__ int listed, number, edge;
-    __shared__ uint32_t bound;
+    __shared__ __align__(16) int bins[R ? BINS : 1];
+    __shared__ float lows[W], total[3];
+    __shared__ int listed, number;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int64_t row = a.row0 + blockIdx.x;
     const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
@@ -292,12 +369,8 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
         for (int r = 0; r < R; ++r) g[r] = r * ROWS_T + t < a.groups ? groups[r * ROWS_T + t] : -INFINITY;
         bins[t] = 0;
     }
-    int32_t token = -1;
-    float logit = 0.f;
-    if (t < a.given) {
-        token = a.tokens[row * a.given + t];
-        if (token >= 0 && token < a.vocab) logit = to_f32(s[token]);
-    }
+    float logit;
+    const int32_t token = load_token<DT>(a, row, logit);
     const float* stretch = a.stretch_stats + 3 * row * a.stretches;
     float m = -INFINITY;
     if (R > 0 || wave == 0) {
@@ -319,8 +392,6 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
             total[1] = sum;
             total[2] = elog;
             listed = number = 0;
-            edge = -1;
-            bound = ~0u;
         }
     }
     if constexpr (R > 0) {
@@ -332,13 +403,7 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
     }
     __syncthreads();
     const RowSums sums(total[0], total[1], total[2]);
-    if (t < a.given) {
-        const bool out = token >= a.vocab;
-        a.logprob[row * a.given + t] = token < 0 ? 0.f : out ? __builtin_nanf("") : sums.log_p(logit, a.inv_temp);
-        if (out && a.dev_status) atomicOr(a.dev_status, MLMC_DEV_RANGE);
-    }
-    if (t == 0 && a.entropy) a.entropy[row] = sums.h;
-    if (a.stats && t < 3) a.stats[3 * row + t] = t == 0 ? sums.m : t == 1 ? sums.log_s : sums.h;
+    write_sums(a, row, token, logit, sums);
     if constexpr (R > 0) {
         if (sums.bad) {
             for (int i = t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
@@ -347,73 +412,43 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
         float low = m;
 #pragma unroll
         for (int w = 0; w < W; ++w) low = fminf(low, lows[w]);
-        const float scale = (BINS - 0.5f) / fminf(m - low, 64.f / a.inv_temp);
+        Bound bound(m, low, a.inv_temp);
         int bin[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {   // not rising with g: a group in a lower bin is greater than one in a higher
-            bin[r] = g[r] == -INFINITY ? BINS : (int)fminf((m - g[r]) * scale, BINS - 1.f);   // (equal groups are all in the last one: fminf takes 0 times infinity for no number)
-            if (bin[r] < BINS) atomicAdd(&bins[bin[r]], 1);
+        for (int r = 0; r < R; ++r) {
+            bin[r] = bound.bin(g[r]);
+            bound.count(bins, bin[r]);
         }
         __syncthreads();
-        const int own = bins[t], prefix = wave_prefix(own);
-        if (lane == 63) totals[wave] = prefix;
-        __syncthreads();
-        int upto = prefix, all = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if (w < wave) upto += totals[w];
-            all += totals[w];
-        }
-        if (upto >= a.top && upto - own < a.top) edge = upto <= LIST ? t : BINS;
-        if (t == 0 && all < a.top) {   // fewer groups than alternatives: all that are not -Inf, and all of their entries
-            edge = BINS - 1;
-            bound = ordered(LOWEST);
-        }
-        __syncthreads();
-        int n;
-        const int last = edge;
-        if (last < BINS) {
+        bound.find(bins, a.top);
+        int n = ROOM + 1;
+        if (bound.upto <= LIST) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (bin[r] <= last) {
-                    list[atomicAdd(&listed, 1)] = r * ROWS_T + t;
-                    atomicMin(&bound, ordered(g[r]));
-                }
+                if (bin[r] <= bound.edge && bin[r] < BINS) list[atomicAdd(&listed, 1)] = r * ROWS_T + t;
             __syncthreads();
-            const int many = listed;
-            const float least = unordered(bound);
+            const float least = bound.least();
             const int each = 64 / a.lanes, mine = lane / a.lanes, place = lane & (a.lanes - 1);
-            for (int i = wave * each; i < many; i += W * each * BATCH) {
+            for (int i = wave * each; i < bound.upto; i += W * each * BATCH) {
                 chunk_t v[BATCH];
                 unsigned col[BATCH];
 #pragma unroll
                 for (int u = 0; u < BATCH; ++u) {
                     const int at = i + u * W * each + mine;
-                    col[u] = at < many ? (list[at] * a.lanes + place) * E : (unsigned)a.vocab;
+                    col[u] = at < bound.upto ? (list[at] * a.lanes + place) * E : (unsigned)a.vocab;
                     v[u] = load_chunk<DT>(s, col[u], a.vocab);   // -Inf past the row's end
                 }
 #pragma unroll
                 for (int u = 0; u < BATCH; ++u) {
                     float f[E];
                     chunk_floats<DT>(f, v[u]);
-                    int hits = 0;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) hits += f[e] >= least;
-                    if (hits) {
-                        int at = atomicAdd(&number, hits);
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (f[e] >= least) {
-                                if (at < ROOM) found[at] = key_of(f[e], col[u] + e);
-                                ++at;
-                            }
-                    }
+                    collect(f, least, col[u], found, &number);
                 }
             }
             __syncthreads();
             n = number;
         }
-        if (last == BINS || n > ROOM) {
+        if (n > ROOM) {
             if (wave == 0) {
                 n = top_by_bisection<DT>(a, s, groups, found, list);
                 if (lane == 0) number = n;
@@ -421,14 +456,115 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
             __syncthreads();
             n = number;
         }
-        for (int i = t; i < n; i += ROWS_T) {
-            const uint64_t key = found[i];
-            int before = 0;
-#pragma unroll 8
-            for (int o = 0; o < n; ++o) before += found[o] > key;
-            if (before < a.top) write_top(a, row, before, key, sums);
+        write_found(a, row, found, n, sums);
+    }
+}
+
+// A short row (up to 1024 chunks of 16 bytes) by a workgroup, all of it in its registers: a chunk is a group, and its entries are at hand.
+template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logprobs_short(LogprobArgs a) {
+    constexpr int E = ENTRIES<DT>, N = SHORT_CHUNKS / ROWS_T, W = ROWS_T / 64;
+    __shared__ uint64_t found[TOP ? ROOM : 1];
+    __shared__ uint32_t list[TOP ? 2 * MOST_ANSWERS : 1];
+    __shared__ float groups[TOP ? SHORT_CHUNKS : 1];
+    __shared__ __align__(16) int bins[TOP ? BINS : 1];
+    __shared__ float most[W], lows[W], part[2][W];
+    __shared__ int number;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, vocab = (int)a.vocab;
+    const int64_t row = a.row0 + blockIdx.x;
+    const entry_t<DT>* s = (const entry_t<DT>*)a.s + row * a.lds;
+    chunk_t v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+        if (n * ROWS_T * E < vocab) v[n] = load_chunk<DT>(s, (n * ROWS_T + t) * E, vocab);
+    float logit;
+    const int32_t token = load_token<DT>(a, row, logit);
+    float f[E], g[N], m = -INFINITY, low = INFINITY;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        g[n] = -INFINITY;
+        if (n * ROWS_T * E >= vocab) continue;
+        chunk_floats<DT>(f, v[n]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) g[n] = fmaxf(g[n], f[e]);
+        m = fmaxf(m, g[n]);
+        if (TOP && g[n] != -INFINITY) low = fminf(low, g[n]);
+    }
+    m = wave_max(m);
+    if (TOP) low = -wave_max(-low);
+    if (lane == 0) {
+        most[wave] = m;
+        lows[wave] = low;
+    }
+    if (TOP) {
+        bins[t] = 0;
+        if (t == 0) number = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        m = fmaxf(m, most[w]);
+        low = fminf(low, lows[w]);
+    }
+    Bound bound(m, low, a.inv_temp);
+    if (TOP) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) bound.count(bins, bound.bin(g[n]));
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+    float sum = 0.f, elog = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n * ROWS_T * E >= vocab) continue;
+        chunk_floats<DT>(f, v[n]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = (f[e] - from) * a.unit, p = __builtin_amdgcn_exp2f(x);
+            sum += p;
+            elog = fmaf(p, fmaxf(x, -1024.f), elog);
         }
-        for (int i = n + t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+    }
+    sum = wave_sum(sum);
+    elog = wave_sum(elog);
+    if (lane == 0) {
+        part[0][wave] = sum;
+        part[1][wave] = elog;
+    }
+    __syncthreads();
+    sum = elog = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        sum += part[0][w];
+        elog += part[1][w];
+    }
+    const RowSums sums(m, sum, elog);
+    write_sums(a, row, token, logit, sums);
+    if constexpr (TOP) {
+        if (sums.bad) {
+            for (int i = t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+            return;
+        }
+        bound.find(bins, a.top);
+        const float least = bound.least();
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (g[n] >= least) {
+                chunk_floats<DT>(f, v[n]);
+                collect(f, least, (unsigned)((n * ROWS_T + t) * E), found, &number);
+            }
+        __syncthreads();
+        int n = number;
+        if (n > ROOM) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) groups[k * ROWS_T + t] = g[k];
+            __syncthreads();
+            if (wave == 0) {
+                n = top_by_bisection<DT>(a, s, groups, found, list);
+                if (lane == 0) number = n;
+            }
+            __syncthreads();
+            n = number;
+        }
+        write_found(a, row, found, n, sums);
     }
 }
 
@@ -545,11 +681,12 @@ struct LogprobPlan { int stretches, groups, lanes; };
 static LogprobPlan logprob_plan(int64_t vocab, int dtype, int top) {
     const int64_t E = dtype == MLMC_BF16 ? 8 : 4, stretch = 64 * STRETCH_N * E, chunks = (vocab + E - 1) / E;
     LogprobPlan p = {(int)((vocab + stretch - 1) / stretch), 0, 1};
+    if (chunks <= SHORT_CHUNKS) return {0, (int)chunks, 1};   // by one workgroup, without a workspace
     while (p.lanes < 64 && (chunks + p.lanes - 1) / p.lanes > GROUPS_MOST) p.lanes *= 2;
     if (top) p.groups = (int)((chunks + p.lanes - 1) / p.lanes);
     return p;
 }
-static size_t logprob_bytes(const LogprobPlan& p, int64_t rows) { return (size_t)rows * ((size_t)p.stretches * 3 + p.groups) * sizeof(float); }
+static size_t logprob_bytes(const LogprobPlan& p, int64_t rows) { return p.stretches == 0 ? 0 : (size_t)rows * ((size_t)p.stretches * 3 + p.groups) * sizeof(float); }
 static bool logprob_sizes_ok(int64_t rows, int64_t vocab, int given, int top) {
     return rows >= 0 && rows < ((int64_t)1 << 31) && vocab >= 1 && vocab <= VOCAB_MAX && given >= 0 && given <= MOST_ANSWERS && top >= 0 && top <= MOST_ANSWERS;
 }
@@ -560,9 +697,13 @@ template <int DT> static mlmc_status logprob_run(LogprobArgs a, hipStream_t st) 
     const int each = a.stretches < STRETCH_WG / 64 ? a.stretches : STRETCH_WG / 64;
     for (; a.row0 < a.rows; a.row0 += ROW_SLICE) {
         const unsigned rows = (unsigned)(a.rows - a.row0 < ROW_SLICE ? a.rows - a.row0 : ROW_SLICE);
+        if (a.stretches == 0) {
+            if (a.top) MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, true><<<rows, ROWS_T, 0, st>>>(a)));
+            else MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, false><<<rows, ROWS_T, 0, st>>>(a)));
+            continue;
+        }
         MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs<DT><<<dim3((unsigned)((a.stretches + each - 1) / each), rows), each * 64, 0, st>>>(a)));
         if (a.groups == 0) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 0><<<rows, ROWS_T, 0, st>>>(a)));
-        else if (a.groups <= ROWS_T) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 1><<<rows, ROWS_T, 0, st>>>(a)));
         else if (a.groups <= 4 * ROWS_T) MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 4><<<rows, ROWS_T, 0, st>>>(a)));
         else MLMC_LAUNCH(K_LOGPROBS_ROWS, st, (k_logprobs_rows<DT, 16><<<rows, ROWS_T, 0, st>>>(a)));
     }
@@ -603,7 +744,7 @@ mlmc_status mlmc_token_logprobs(const void* logits, int64_t ldl, int64_t rows, i
     }
     const LogprobPlan p = logprob_plan(vocab, dtype, top);
     const size_t need = logprob_bytes(p, rows);
-    if (rows > 0 && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
+    if (rows > 0 && need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     if (dev_status) MLMC_LAUNCH(K_ZERO, st, (k_logprobs_clear<<<1, 1, 0, st>>>(dev_status)));
     if (rows == 0) return MLMC_OK;
     LogprobArgs a = {};

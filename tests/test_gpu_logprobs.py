@@ -219,8 +219,10 @@ def test_large_temperatures_and_logits():
 
 
 def test_kernels():
-    x = torch.zeros((600, 1000), device="cuda")
-    assert launched(lambda: P.mlmc_token_logprobs(x, top=3)) == {"k_logprobs", "k_logprobs_rows"}
+    """A workgroup has a short row, longer ones take two launches."""
+    x, y = torch.zeros((600, 4096), device="cuda"), torch.zeros((2, 4097), device="cuda")
+    assert P.mlmc_token_logprobs_workspace(600, 4096, 3) == 0 and launched(lambda: P.mlmc_token_logprobs(x, top=3)) == {"k_logprobs"}
+    assert launched(lambda: P.mlmc_token_logprobs(y, top=3)) == launched(lambda: P.mlmc_token_logprobs(y)) == {"k_logprobs", "k_logprobs_rows"}
     assert launched(lambda: P.mlmc_token_logprobs_backward(x, torch.zeros((600, 3), device="cuda"))) == {"k_logprobs_backward"}
 
 
