@@ -360,40 +360,57 @@ __global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 
     FA.init(wm * FM);
     FB.init(wn * FN);
     constexpr int Q = PIECES<DT>;
-    fragment_t<DT> fa[2][FM], fb[2][FN];
+    // Fragments of two pieces.  Those of 8 bits have twice the registers: a fragment of A is read over as soon as its instructions have gone out (two of each: 424 registers spilled).
+    constexpr int PAIR = DT == DT_E4M3 ? 1 : 2;
+    fragment_t<DT> fa[PAIR][FM], fb[2][FN];
+    const auto read_a = [&](const chunk_t* sa, int m, int q) { fa[q & (PAIR - 1)][m] = FA.get(sa, m, q); };
+    const auto read_b = [&](const chunk_t* sb, int n, int q) { fb[q & 1][n] = FB.get(sb, n, q); };
     const auto read = [&](const chunk_t* sa, const chunk_t* sb, int q) {
 #pragma unroll
-        for (int m = 0; m < FM; ++m) fa[q & 1][m] = FA.get(sa, m, q);
+        for (int m = 0; m < FM; ++m) read_a(sa, m, q);
 #pragma unroll
-        for (int n = 0; n < FN; ++n) fb[q & 1][n] = FB.get(sb, n, q);
+        for (int n = 0; n < FN; ++n) read_b(sb, n, q);
     };
-    const auto multiply_quarter = [&](int q) {
-#pragma unroll
-        for (int m = 0; m < FM; ++m)
-#pragma unroll
-            for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
-        // the reads and the loads between the matrix instructions: left alone they sink behind them
+    // The products of piece q; piece `next` of a pair of buffers is read meanwhile, if there is more.
+    const auto multiply_piece = [&](int q, auto more, const chunk_t* sa, const chunk_t* sb, int next) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(more)::value;
         if constexpr (DT == DT_E4M3) {
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+                if (MORE) read_b(sb, n, next);
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+#pragma unroll
+                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[0][m], acc[m][n]);
+                if (MORE) read_a(sa, m, next);
+            }
             constexpr int READS = 2 * (FM + FN), EACH = (READS + FM * FN - 1) / (FM * FN);
 #pragma unroll
             for (int i = 0; i < FM * FN; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
                 if (FAST) __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
-            return;
-        }
-        constexpr int READS = FM * (AA ? 1 : DT == MLMC_BF16 ? 2 : 4) + FN * (BA ? 1 : DT == MLMC_BF16 ? 2 : 4);
+        } else {
+            if (MORE) read(sa, sb, next);
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            if (FAST && (q == 3 || q == 0)) __builtin_amdgcn_sched_group_barrier(0x10, WAY == WAY_WORDS ? 4 : 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<DT>(fb[q & 1][n], fa[q & 1][m], acc[m][n]);
+            // the reads and the loads between the matrix instructions: left alone they sink behind them
+            constexpr int READS = FM * (AA ? 1 : DT == MLMC_BF16 ? 2 : 4) + FN * (BA ? 1 : DT == MLMC_BF16 ? 2 : 4);
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (FAST && (q == 3 || q == 0)) __builtin_amdgcn_sched_group_barrier(0x10, WAY == WAY_WORDS ? 4 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
     };
+    constexpr std::true_type there_is_more;
     const auto add_rows = [&](const chunk_t* sa) {
         if constexpr (!AA)
             if (rows)
@@ -421,9 +438,8 @@ __global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 
         }
 #pragma unroll
         for (int q = 0; q < Q - 1; ++q) {
-            read(sa, sb, q + 1);
             if (FAST && q == 0) B.fetch(nb, c + STEP, c_whole);
-            multiply_quarter(q);
+            multiply_piece(q, there_is_more, sa, sb, q + 1);
         }
         add_rows(sa);
         if constexpr (!FAST) {
@@ -432,8 +448,7 @@ __global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 
         }
         arrived();
         if constexpr (FAST) A.fetch(sa, c + 2 * STEP, c_whole);
-        read(na, nb, 0);
-        multiply_quarter(Q - 1);
+        multiply_piece(Q - 1, there_is_more, na, nb, 0);
     };
     const auto guarded = [&](int c, chunk_t* sa, chunk_t* sb) {
         chunk_t va[OpA::N], vb[OpB::N];
@@ -464,8 +479,8 @@ __global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 
         read(a0, b0, 0);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            if (q < Q - 1) read(a0, b0, q + 1);
-            multiply_quarter(q);
+            if (q < Q - 1) multiply_piece(q, there_is_more, a0, b0, q + 1);
+            else multiply_piece(q, std::false_type{}, a0, b0, 0);
         }
         add_rows(a0);
         arrived();
