@@ -622,29 +622,41 @@ def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
     ldx = _matrix(x, "x")
     dtype = x.dtype
     n, d = x.shape
-    p_r, ldr = _or_none(residual, "residual", dtype, n, d)
-    if residual is None:
-        if sum is not None:
-            raise MlmcError("sum is an output of a norm with a residual")
-    elif sum is None:
-        sum = x.new_empty((n, d))
-    if y is None and with_y:
-        y = x.new_empty((n, d))
-    if q is None and with_q:
-        q = _eight_bits(n, d, x)
-    if q is not None and scale is None:
-        scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    if q is None and scale is not None:
+    p_r = p_s = p_y = p_q = p_scale = p_rstd = None     # what the call makes itself needs no check
+    ldr = lds = ldy = ldq = 0
+    if residual is not None:
+        p_r, ldr = residual.data_ptr(), _matrix(residual, "residual", dtype, n, d)
+        if sum is None:
+            sum, lds = x.new_empty((n, d)), d
+        else:
+            lds = _matrix(sum, "sum", dtype, n, d)
+        p_s = sum.data_ptr()
+    elif sum is not None:
+        raise MlmcError("sum is an output of a norm with a residual")
+    if y is not None:
+        p_y, ldy = y.data_ptr(), _matrix(y, "y", dtype, n, d)
+    elif with_y:
+        y, ldy = x.new_empty((n, d)), d
+        p_y = y.data_ptr()
+    if q is not None or with_q:
+        if q is None:
+            q = _eight_bits(n, d, x)
+        p_q, ldq = q.data_ptr(), _matrix(q, "q", _E4M3, n, d)
+        if scale is None:
+            scale = torch.empty(n, dtype=torch.float32, device=x.device)
+            p_scale = scale.data_ptr()
+        else:
+            p_scale = _vector(scale, "scale", n)
+    elif scale is not None:
         raise MlmcError("scale is that of q")
-    if y is None and q is None:
+    elif y is None:
         raise MlmcError("neither y nor q is asked for")
-    if rstd is None and with_rstd:
+    if rstd is not None:
+        p_rstd = _vector(rstd, "rstd", n)
+    elif with_rstd:
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-    p_s, lds = _or_none(sum, "sum", dtype, n, d)
-    p_y, ldy = _or_none(y, "y", dtype, n, d)
-    p_q, ldq = _or_none(q, "q", _E4M3, n, d)
-    rc = lib().mlmc_rms_norm(x.data_ptr(), ldx, p_r, ldr, n, d, _DTYPE[dtype], _vector(weight, "weight", d), eps, p_s, lds, p_y, ldy, p_q, ldq,
-                             _vector(scale, "scale", n), _vector(rstd, "rstd", n), _stream())
+        p_rstd = rstd.data_ptr()
+    rc = lib().mlmc_rms_norm(x.data_ptr(), ldx, p_r, ldr, n, d, _DTYPE[dtype], _vector(weight, "weight", d), eps, p_s, lds, p_y, ldy, p_q, ldq, p_scale, p_rstd, _stream())
     if rc:
         _check(rc, "mlmc_rms_norm")
     return RmsNorm(y, sum, rstd, q, scale)

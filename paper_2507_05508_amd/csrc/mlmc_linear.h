@@ -692,7 +692,7 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
         if (t == TILE_256 && (dtype == MLMC_F32 || !fast)) continue;
         const TileCost& k = tile_costs[t];
         const int64_t tiles = ((I + k.rows - 1) / k.rows) * ((J + k.cols - 1) / k.cols);
-        for (int s = 1; s <= SPLITS_MAX && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
+        for (int s = 1; s <= (dtype == DT_E4M3 && t == TILE_256 ? 1 : SPLITS_MAX) && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
             const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
             if (parts != s) continue;
             const float us = LAUNCH_US + (float)rounds * (k.round_us + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
@@ -771,8 +771,11 @@ template <int DT> __global__ __launch_bounds__(256) void k_linear_pack(PackArgs 
     p.to[which][t] = cut_chunk<DT, true>(v, r, p.rows[which], (int64_t)c * E, p.cols[which]);
 }
 
+static mlmc_status linear_q8_big(LinearArgs& g, hipStream_t st);   // mlmc_linear_q8.hip
 template <int DT, bool AA, bool BA, int WAY> static mlmc_status linear_tile(LinearArgs& g, int tile, hipStream_t st) {
-    if constexpr (DT != MLMC_F32 && WAY == WAY_CHUNKS)
+    if constexpr (DT == DT_E4M3 && WAY == WAY_CHUNKS)
+        if (tile == TILE_256) return linear_q8_big(g, st);
+    if constexpr (DT == MLMC_BF16 && WAY == WAY_CHUNKS)
         if (tile == TILE_256) return launch_tile<DT, 2, 4, 4, 2, AA, BA, WAY>(g, st);
     if (tile == TILE_128) return launch_tile<DT, 2, 2, 2, 2, AA, BA, WAY>(g, st);
     if (tile == TILE_64) return launch_tile<DT, 1, 4, 2, 1, AA, BA, WAY>(g, st);

@@ -6,6 +6,218 @@
 // Accumulators are fp32.
 #include "mlmc_linear.h"
 
+namespace mlmc {
+
+// The large tile of matrices whose rows are aligned: 256 x 256 by 4 waves of 128 x 128, a workgroup for every CU with tile after tile, the first loads of the next one ahead of the stores of the last.
+// Loads and barriers as in k_linear_tile; a wave's fragments of the next half step are read over those of this one, A's as soon as its instructions have gone out.
+// 8192 x 4096 x 4096: by 8 waves of 128 x 64 (k_linear_tile) 148 us; by two workgroups a CU, 128 x 256 each and steps of 64 bytes, 186: the matrix units take 1.55 us a step at the clock that
+// they leave the card, and half as much again from the L2 makes that 2.5.
+constexpr int BIG = 256, BIG_T = 256, BIG_F = 4;
+using v2b = __bf16 __attribute__((ext_vector_type(2)));
+using v4b = __bf16 __attribute__((ext_vector_type(4)));
+using v4b_u = __bf16 __attribute__((ext_vector_type(4), aligned(2)));   // at any entry's place
+__global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
+    using Op = Operand<DT_E4M3, true, BIG, BIG_T, WAY_CHUNKS>;
+    constexpr int STEP = Op::STEP, F = BIG_F;
+    __shared__ chunk_t a0[BIG * 8], b0[BIG * 8], a1[BIG * 8], b1[BIG * 8];
+    __shared__ __align__(16) float scales[BIG], biases[BIG];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1, half = lane >> 5;
+    const auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int tiles = g.tiles_i * g.tiles_j, C = (int)g.C, c_whole = C - C % STEP;
+    Op A, B;
+    int64_t i0, j0;
+    const auto place = [&](int k) {   // neighbouring tiles to the workgroups of one die (workgroups go round the 8 dies), eight tile rows at a time
+        const int q = tiles / 8, r = tiles % 8, x = k & 7, t = x * q + (x < r ? x : r) + (k >> 3);
+        const int band = uniform(t / (8 * g.tiles_j)), in_band = t - band * 8 * g.tiles_j, high = min(8, g.tiles_i - band * 8);
+        const int tj = uniform(in_band / high), ti = band * 8 + in_band - tj * high;
+        i0 = (int64_t)ti * BIG;
+        j0 = (int64_t)tj * BIG;
+        A.init(g.a, g.lda, i0, g.I, g.C);
+        B.init(g.b, g.ldb, j0, g.J, g.C);
+    };
+    v16f acc[F][F];
+    Fragments<DT_E4M3, true, BIG, F> FA, FB;
+    FA.init(wm * F);
+    FB.init(wn * F);
+    v8i fa[F], fb[2][F];
+    const auto read = [&](const chunk_t* sa, const chunk_t* sb) {
+#pragma unroll
+        for (int n = 0; n < F; ++n) fb[0][n] = FB.get(sb, n, 0);
+#pragma unroll
+        for (int m = 0; m < F; ++m) fa[m] = FA.get(sa, m, 0);
+    };
+    // the products of half q of a step; the other half of a pair of buffers is read meanwhile, if there is more
+    const auto multiply_half = [&](int q, auto more, const chunk_t* sa, const chunk_t* sb) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(more)::value;
+#pragma unroll
+        for (int n = 0; n < F; ++n)
+            if (MORE) fb[1 - q][n] = FB.get(sb, n, 1 - q);
+#pragma unroll
+        for (int m = 0; m < F; ++m) {
+#pragma unroll
+            for (int n = 0; n < F; ++n) acc[m][n] = multiply<DT_E4M3>(fb[q][n], fa[m], acc[m][n]);
+            if (MORE) fa[m] = FA.get(sa, m, 1 - q);
+        }
+#pragma unroll
+        for (int i = 0; i < F * F; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::true_type more;
+    const auto arrived = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): also what goes to LDS by itself
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const auto step = [&](int c, chunk_t* sa, chunk_t* sb, chunk_t* na, chunk_t* nb) {
+        B.fetch(nb, c + STEP, c_whole);
+        multiply_half(0, more, sa, sb);
+        arrived();
+        A.fetch(sa, c + 2 * STEP, c_whole);
+        multiply_half(1, more, na, nb);
+    };
+    int k = blockIdx.x;
+    place(k);
+    A.fetch(a0, 0, c_whole);
+    B.fetch(b0, 0, c_whole);
+    while (true) {
+        {
+            const int64_t j = min(j0 + threadIdx.x, g.J - 1);
+            scales[threadIdx.x] = g.col_scale[j];
+            biases[threadIdx.x] = g.bias ? g.bias[j] : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < F; ++m)
+#pragma unroll
+            for (int n = 0; n < F; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
+        arrived();
+        A.fetch(a1, STEP, c_whole);
+        read(a0, b0);
+        int c = 0;
+        for (; c + STEP < c_whole; c += 2 * STEP) {
+            step(c, a0, b0, a1, b1);
+            step(c + STEP, a1, b1, a0, b0);
+        }
+        if (c < c_whole) step(c, a0, b0, a1, b1);
+        arrived();
+        if (c_whole < C) {   // a step that is not whole
+            chunk_t v[Op::N];
+            A.load(v, c_whole);
+            A.store(a0, v, c_whole);
+            B.load(v, c_whole);
+            B.store(b0, v, c_whole);
+            arrived();
+            read(a0, b0);
+            multiply_half(0, more, a0, b0);
+            multiply_half(1, std::false_type{}, a0, b0);
+            arrived();
+        }
+        const int64_t oi = i0 + wm * 128 + (lane & 31), oj = j0 + wn * 128;
+        float rs[F];   // ahead of the next tile's loads: what is waited for comes in order
+#pragma unroll
+        for (int m = 0; m < F; ++m) rs[m] = g.row_scale[min(oi + m * 32, g.I - 1)];
+        k += gridDim.x;
+        const bool again = k < tiles;
+        if (again) {
+            place(k);
+            A.fetch(a0, 0, c_whole);
+            B.fetch(b0, 0, c_whole);
+        }
+        // A lane has four neighbouring entries of a row in four registers (the operands are exchanged): rounded and exchanged between the halves of the wave they are eight, 16 bytes.  (By way of the
+        // second buffers, 256 bytes of each of four rows a store, the waits of the one wave a SIMD took more than the fuller lines gave: 154 us instead of 139.)
+        const auto results = [&](auto act, auto whole) __attribute__((always_inline)) {
+            constexpr int ACT = decltype(act)::value;
+            constexpr bool WHOLE = decltype(whole)::value;   // all columns of the tile
+#pragma unroll
+            for (int n = 0; n < F; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) {
+                    v4f cs[2], bs[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int at = wn * 128 + n * 32 + (q + h) * 8 + half * 4;
+                        cs[h] = *(const v4f*)(scales + at);
+                        bs[h] = *(const v4f*)(biases + at);
+                    }
+                    const int64_t j = oj + n * 32 + (q + half) * 8;   // of the eight that the lane stores
+#pragma unroll
+                    for (int m = 0; m < F; ++m) {
+                        const int64_t i = oi + m * 32;
+                        unsigned packed[2][2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                v[e] = fmaf(acc[m][n][(q + h) * 4 + e] * rs[m], cs[h][e], bs[h][e]);
+                                if (ACT == MLMC_ACT_GELU) v[e] = gelu<MLMC_BF16>(v[e]);
+                                if (ACT == MLMC_ACT_RELU) v[e] = relu(v[e]);
+                            }
+                            if (g.residual) {
+                                const int64_t jr = oj + n * 32 + (q + h) * 8 + half * 4;
+                                const __bf16* r = (const __bf16*)g.residual + min(i, g.I - 1) * g.ldr + jr;
+                                if (WHOLE) {
+                                    const v4b u = *(const v4b_u*)r;
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) v[e] += (float)u[e];
+                                } else {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        if (jr + e < g.J) v[e] += (float)r[e];
+                                }
+                            }
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) packed[h][w] = __builtin_bit_cast(unsigned, v2b{(__bf16)v[2 * w], (__bf16)v[2 * w + 1]});
+                        }
+                        chunk_t out;
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {   // lanes 0 to 31 get the first eight, the others the second
+                            const auto both = __builtin_amdgcn_permlane32_swap(packed[0][w], packed[1][w], false, false);
+                            out[w] = (int)both[0];
+                            out[2 + w] = (int)both[1];
+                        }
+                        if (i >= g.I) continue;
+                        __bf16* y = (__bf16*)g.out + i * g.ldo + j;
+                        if (WHOLE) *(chunk_u*)y = out;
+                        else {
+                            const v8b u = __builtin_bit_cast(v8b, out);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (j + e < g.J) y[e] = u[e];
+                        }
+                    }
+                }
+        };
+        const auto results_of = [&](auto act) __attribute__((always_inline)) {
+            if (oj - wn * 128 + BIG <= g.J) results(act, std::true_type{});
+            else results(act, std::false_type{});
+        };
+        if (g.act == MLMC_ACT_GELU) results_of(std::integral_constant<int, MLMC_ACT_GELU>{});
+        else if (g.act == MLMC_ACT_RELU) results_of(std::integral_constant<int, MLMC_ACT_RELU>{});
+        else results_of(std::integral_constant<int, MLMC_ACT_NONE>{});
+        if (!again) return;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();   // scales and biases have been read
+        asm volatile("" ::: "memory");
+    }
+}
+
+static mlmc_status linear_q8_big(LinearArgs& g, hipStream_t st) {
+    g.tiles_i = (int)((g.I + BIG - 1) / BIG);
+    g.tiles_j = (int)((g.J + BIG - 1) / BIG);
+    const int tiles = g.tiles_i * g.tiles_j;
+    MLMC_LAUNCH(K_LINEAR_Q8, st, (k_linear_q8<<<tiles < LINEAR_CUS ? tiles : LINEAR_CUS, BIG_T, 0, st>>>(g)));
+    return MLMC_OK;
+}
+
+}  // namespace mlmc
+
 using namespace mlmc;
 
 extern "C" {
