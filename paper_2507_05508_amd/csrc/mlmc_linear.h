@@ -257,11 +257,12 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
     using L = Lds<DT, ALONG, T>;
     __device__ static int row(int q) { return q / L::W; }
     __device__ static int chunk(int q) { return (q % L::W) ^ L::swizzle(q / L::W); }   // which chunk of the row slot q holds
-    __device__ void init(const void* p_, int64_t ld_, int64_t i0_, int64_t I_, int64_t C_) {
+    __device__ void init(const void* p_, int64_t ld_, int64_t i0_, int64_t I_, int64_t C_) { init(p_, ld_, i0_, I_, C_, threadIdx.x); }
+    __device__ void init(const void* p_, int64_t ld_, int64_t i0_, int64_t I_, int64_t C_, int thread) {
         p = p_; ld = ld_; i0 = i0_; I = I_; C = C_;
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int at = u * NT + threadIdx.x, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? (at & 3) * (E / 4) : 0), e = WAY == WAY_WORDS ? E / 4 : E;
+            const int at = u * NT + thread, q = WAY == WAY_WORDS ? at >> 2 : at, r = row(q), c = chunk(q) * E + (WAY == WAY_WORDS ? (at & 3) * (E / 4) : 0), e = WAY == WAY_WORDS ? E / 4 : E;
             // what lies past the matrix repeats its last entries: it reaches only results that are not stored
             if (ALONG) off[u] = (off_t)(((i0 + r < I ? r : I - 1 - i0) * ld + c) * (16 / E));
             else off[u] = (off_t)((r * ld + (i0 + c < I ? c : (I - 1) / e * e - i0)) * (16 / E));
@@ -278,6 +279,17 @@ template <int DT, bool ALONG, int T, int NT, int WAY> struct Operand {
         for (int u = 0; u < LOADS; ++u) {
             if constexpr (WAY == WAY_WORDS) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)((int*)s + u * NT + wave0), 4, (int)off[u], 0, 0, 0);
             else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, (int)off[u], 0, 0, 0);
+        }
+    }
+    // the chunks of a step of which `left` bytes are left, along the contraction; zeros in the place of those that it cuts (their offsets lie outside the buffer)
+    __device__ void fetch_rest(chunk_t* s, int c, int left, int thread) const {
+        static_assert(ALONG && WAY == WAY_CHUNKS, "rows of aligned chunks");
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)p + (i0 * ld + c) * (16 / E), 0, 0x7fffffff, 0x00027000);   // a tile's offsets are below 2^30
+        const int wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x) & ~63;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const bool whole = chunk(u * NT + thread) * 16 + 16 <= left;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + u * NT + wave0), 16, whole ? (int)off[u] : (int)0xc0000000, 0, 0, 0);
         }
     }
     // any step, by way of registers, zeros outside
@@ -675,6 +687,8 @@ enum LinearTile { TILE_32 = 0, TILE_64, TILE_128, TILE_256, TILES };
 struct TileCost { int rows, cols; float alone_us[2], among_us[2], round_us; };   // [dtype]
 constexpr TileCost tile_costs[TILES] = {{32, 128, {0.55f, 0.42f}, {0.53f, 0.28f}, 0.7f}, {64, 128, {0.95f, 0.44f}, {0.95f, 0.33f}, 1.3f},
                                         {128, 128, {1.85f, 0.70f}, {1.85f, 0.50f}, 2.5f}, {256, 256, {0.f, 1.50f}, {0.f, 1.60f}, 11.f}};
+// The large tile of 8 bits has its results stored by one wave a SIMD: 8192 x 4096 x 1024 62 us, by tiles of 128 54; 8192 x 8192 x 2048 158 and 162; 16384 x 1024 x 1024 28 and 29; 4096 x 4096 x 4096 65 and 69.
+constexpr float Q8_BIG_ROUND_US = 15.f;
 constexpr float LAUNCH_US = 5.f, JOIN_US = 3.f, JOIN_ENTRY_US = 1.6e-6f;
 constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
 
@@ -695,7 +709,7 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
         for (int s = 1; s <= (dtype == DT_E4M3 && t == TILE_256 ? 1 : SPLITS_MAX) && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
             const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
             if (parts != s) continue;
-            const float us = LAUNCH_US + (float)rounds * (k.round_us + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
+            const float us = LAUNCH_US + (float)rounds * ((dtype == DT_E4M3 && t == TILE_256 ? Q8_BIG_ROUND_US : k.round_us) + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
                              (s > 1 ? JOIN_US + JOIN_ENTRY_US * (float)(s * I) * (float)J : 0.f);
             if (us < least) {
                 least = us;

@@ -12,7 +12,7 @@ namespace mlmc {
 // Loads and barriers as in k_linear_tile; a wave's fragments of the next half step are read over those of this one, A's as soon as its instructions have gone out.
 // 8192 x 4096 x 4096: by 8 waves of 128 x 64 (k_linear_tile) 148 us; by two workgroups a CU, 128 x 256 each and steps of 64 bytes, 186: the matrix units take 1.55 us a step at the clock that
 // they leave the card, and half as much again from the L2 makes that 2.5.
-constexpr int BIG = 256, BIG_T = 256, BIG_F = 4;
+constexpr int BIG = 256, BIG_T = 256, BIG_F = 4;   // (a thread for every row of the tile)
 using v2b = __bf16 __attribute__((ext_vector_type(2)));
 using v4b = __bf16 __attribute__((ext_vector_type(4)));
 using v4b_u = __bf16 __attribute__((ext_vector_type(4), aligned(2)));   // at any entry's place
@@ -23,6 +23,11 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
     __shared__ __align__(16) float scales[BIG], biases[BIG];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1, half = lane >> 5;
     const auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const auto fresh_thread = [] {   // what follows from it is not kept in registers through the loop
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return t;
+    };
     const int tiles = g.tiles_i * g.tiles_j, C = (int)g.C, c_whole = C - C % STEP;
     Op A, B;
     int64_t i0, j0;
@@ -32,8 +37,9 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         const int tj = uniform(in_band / high), ti = band * 8 + in_band - tj * high;
         i0 = (int64_t)ti * BIG;
         j0 = (int64_t)tj * BIG;
-        A.init(g.a, g.lda, i0, g.I, g.C);
-        B.init(g.b, g.ldb, j0, g.J, g.C);
+        const int thread = fresh_thread();
+        A.init(g.a, g.lda, i0, g.I, g.C, thread);
+        B.init(g.b, g.ldb, j0, g.J, g.C, thread);
     };
     v16f acc[F][F];
     Fragments<DT_E4M3, true, BIG, F> FA, FB;
@@ -107,12 +113,17 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         if (c < c_whole) step(c, a0, b0, a1, b1);
         arrived();
         if (c_whole < C) {   // a step that is not whole
-            chunk_t v[Op::N];
-            A.load(v, c_whole);
-            A.store(a0, v, c_whole);
-            B.load(v, c_whole);
-            B.store(b0, v, c_whole);
+            const int t = fresh_thread();
+            const int left = C - c_whole, cut = c_whole + left / 16 * 16, slot = Op::L::slot(t, left / 16);
+            A.fetch_rest(a0, c_whole, left, t);
+            B.fetch_rest(b0, c_whole, left, t);
             arrived();
+            if (left % 16) {   // the chunk that the end cuts, a row a thread
+                const chunk_t u = raw_chunk<DT_E4M3, true>(g.a, g.lda, i0 + t, g.I, cut, C), v = raw_chunk<DT_E4M3, true>(g.b, g.ldb, j0 + t, g.J, cut, C);
+                a0[slot] = cut_chunk<DT_E4M3, true>(u, i0 + t, g.I, cut, C);
+                b0[slot] = cut_chunk<DT_E4M3, true>(v, j0 + t, g.J, cut, C);
+                arrived();
+            }
             read(a0, b0);
             multiply_half(0, more, a0, b0);
             multiply_half(1, std::false_type{}, a0, b0);

@@ -18,6 +18,7 @@ SIZES = [  # rows, outputs, inputs, pad, shift
     (1, 1, 1, 0, 0), (1, 3, 5, 1, 1), (2, 17, 15, 0, 0), (3, 16, 16, 0, 0), (5, 33, 64, 0, 0), (1, 128, 257, 0, 0), (16, 100, 1000, 8, 0), (16, 4096, 4096, 0, 0), (1, 4096, 4096, 0, 0),
     (17, 64, 128, 0, 0), (33, 65, 127, 1, 3), (40, 129, 130, 0, 0), (64, 128, 512, 0, 0), (100, 200, 300, 5, 0), (129, 257, 1023, 0, 0), (255, 256, 1024, 16, 16), (256, 512, 8192, 0, 0),
     (300, 1000, 13, 0, 0), (513, 1025, 2049, 0, 0), (1000, 640, 4096, 0, 4), (2048, 2048, 1024, 0, 0), (2049, 2305, 1025, 3, 1), (4096, 4096, 512, 0, 0), (4100, 4000, 640, 0, 0), (37, 8192, 96, 0, 0),
+    (4000, 4001, 1072, 0, 0), (4000, 4001, 1071, 1, 0), (3000, 4100, 513, 15, 0), (8200, 2050, 127, 1, 0), (4000, 4000, 112, 16, 0),   # the large tile with what a step of 128 leaves over
 ]
 
 
