@@ -306,19 +306,23 @@ struct Bound {
     __device__ float least() const { return edge >= BINS - 1 ? LOWEST : fmaxf(m - (edge + 1.01f) / scale - fabsf(m) * 0x1p-22f, LOWEST); }
 };
 
-// Entries of a thread's chunk that reach `least`, into `found` as far as there is room.
-template <int E> __device__ inline void collect(const float (&f)[E], float least, unsigned col, uint64_t* found, int* number) {
+// Entries of a thread's chunks that reach `least`, into `found` as far as there is room.
+template <int N, int E> __device__ inline void collect(const float (&f)[N][E], float least, const unsigned (&col)[N], uint64_t* found, int* number) {
     int hits = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) hits += f[e] >= least;
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < E; ++e) hits += f[n][e] >= least;
     if (!hits) return;
     int at = atomicAdd(number, hits);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (f[e] >= least) {
-            if (at < ROOM) found[at] = key_of(f[e], col + e);
-            ++at;
-        }
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (f[n][e] >= least) {
+                if (at < ROOM) found[at] = key_of(f[n][e], col[n] + e);
+                ++at;
+            }
 }
 // The n keys found, each at its place.
 __device__ inline void write_found(const LogprobArgs& a, int64_t row, const uint64_t* found, int n, const RowSums& sums) {
@@ -423,9 +427,13 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
         bound.find(bins, a.top);
         int n = ROOM + 1;
         if (bound.upto <= LIST) {
+            int takes = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) takes += bin[r] <= bound.edge && bin[r] < BINS;
+            int at = takes ? atomicAdd(&listed, takes) : 0;
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (bin[r] <= bound.edge && bin[r] < BINS) list[atomicAdd(&listed, 1)] = r * ROWS_T + t;
+                if (bin[r] <= bound.edge && bin[r] < BINS) list[at++] = r * ROWS_T + t;
             __syncthreads();
             const float least = bound.least();
             const int each = 64 / a.lanes, mine = lane / a.lanes, place = lane & (a.lanes - 1);
@@ -438,12 +446,10 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
                     col[u] = at < bound.upto ? (list[at] * a.lanes + place) * E : (unsigned)a.vocab;
                     v[u] = load_chunk<DT>(s, col[u], a.vocab);   // -Inf past the row's end
                 }
+                float f[BATCH][E];
 #pragma unroll
-                for (int u = 0; u < BATCH; ++u) {
-                    float f[E];
-                    chunk_floats<DT>(f, v[u]);
-                    collect(f, least, col[u], found, &number);
-                }
+                for (int u = 0; u < BATCH; ++u) chunk_floats<DT>(f[u], v[u]);
+                collect(f, least, col, found, &number);
             }
             __syncthreads();
             n = number;
@@ -545,12 +551,23 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
         }
         bound.find(bins, a.top);
         const float least = bound.least();
+        float most_here = g[0];
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-            if (g[n] >= least) {
-                chunk_floats<DT>(f, v[n]);
-                collect(f, least, (unsigned)((n * ROWS_T + t) * E), found, &number);
+        for (int n = 1; n < N; ++n) most_here = fmaxf(most_here, g[n]);
+        if (most_here >= least) {
+            float all[N][E];
+            unsigned col[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                col[n] = (unsigned)((n * ROWS_T + t) * E);
+                if (n * ROWS_T * E < vocab) chunk_floats<DT>(all[n], v[n]);
+                else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) all[n][e] = -INFINITY;
+                }
             }
+            collect(all, least, col, found, &number);
+        }
         __syncthreads();
         int n = number;
         if (n > ROOM) {

@@ -27,6 +27,8 @@ struct RmsArgs {
     float *scale, *rstd;
     float* part;          // [groups][d] sums of a group's rows
     int64_t groups;
+    void* dweight;        // written by the only group, if there is no more than one
+    int grad_dtype;
 };
 
 constexpr float E4M3_MAX = 448.f, LEAST_SCALE = 0x1p-100f;
@@ -169,6 +171,12 @@ template <int DT, int T, int P, int WG, bool NORM, bool RES> __global__ __launch
     }
 }
 
+__device__ inline void sum_of_group(const RmsArgs& a, int64_t group, int64_t j, float v) {
+    if (a.part) a.part[group * a.d + j] = v;
+    else if (a.grad_dtype == MLMC_F32) ((float*)a.dweight)[j] = v;
+    else ((__bf16*)a.dweight)[j] = (__bf16)v;
+}
+
 // The gradient, in workgroups of 1024 threads, one for every CU: dy and s are read once, a thread's columns of dweight are added up in its registers over all its rows, then over the
 // workgroup's rows in LDS, and a workgroup leaves one partial sum for k_norm_join.
 template <int DT, int T, int P, int WG, bool RES> __global__ __launch_bounds__(WG) void k_rms_backward_rows(RmsArgs a) {
@@ -226,7 +234,7 @@ template <int DT, int T, int P, int WG, bool RES> __global__ __launch_bounds__(W
         }
         of.store((entry_t<DT>*)a.dx + row * a.lddx, c);
     }
-    if (!a.part) return;
+    if (!a.part && !a.dweight) return;
     if constexpr (R > 1) {   // the sub-rows' sums one after the other
         for (int r = 0; r < R; ++r) {
             if (sub == r) {
@@ -242,11 +250,10 @@ template <int DT, int T, int P, int WG, bool RES> __global__ __launch_bounds__(W
         }
         if (sub != R - 1) return;
     }
-    float* p = a.part + (int64_t)blockIdx.x * a.d;
 #pragma unroll
     for (int e = 0; e < P; ++e) {
         const int j = of.at(e);
-        if (j < of.d) p[j] = dw[e];
+        if (j < of.d) sum_of_group(a, blockIdx.x, j, dw[e]);
     }
 }
 
@@ -312,7 +319,7 @@ template <int DT> __global__ __launch_bounds__(RMS_WG) void k_rms_columns(RmsArg
     float dw = 0.f;
     for (int64_t i = blockIdx.y; i < a.rows; i += a.groups)
         dw = fmaf(to_f32(((const entry_t<DT>*)a.dy)[i * a.lddy + j]), to_f32(((const entry_t<DT>*)a.x)[i * a.ldx + j]) * a.rstd_in[i], dw);
-    a.part[(int64_t)blockIdx.y * a.d + j] = dw;
+    sum_of_group(a, blockIdx.y, j, dw);
 }
 
 template <int DT, int T, int P, bool NORM> static mlmc_status rms_forward_rows(const RmsArgs& a, hipStream_t st) {
@@ -348,7 +355,7 @@ template <int DT, int T, int P> static mlmc_status rms_backward_rows(const RmsAr
 template <int DT> static mlmc_status rms_backward(RmsArgs a, hipStream_t st) {
     if (a.d < NORM_ROW_MIN || a.d > NORM_ROW_MAX) {
         const dim3 grid((unsigned)((a.d + RMS_WG - 1) / RMS_WG), (unsigned)a.groups);
-        if (a.part) MLMC_LAUNCH(K_RMS_COLUMNS, st, (k_rms_columns<DT><<<grid, RMS_WG, 0, st>>>(a)));
+        if (a.part || a.dweight) MLMC_LAUNCH(K_RMS_COLUMNS, st, (k_rms_columns<DT><<<grid, RMS_WG, 0, st>>>(a)));
         for (; a.row0 < a.rows; a.row0 += RMS_SLICE) MLMC_LAUNCH(K_RMS_BACKWARD, st, (k_rms_backward<DT><<<rms_slice(a), RMS_WG, 0, st>>>(a)));
         return MLMC_OK;
     }
@@ -368,7 +375,8 @@ using namespace mlmc;
 extern "C" {
 
 size_t mlmc_rms_norm_workspace(int64_t rows, int64_t d) {
-    return norm_sizes_ok(rows, d) ? (size_t)norm_groups(rows, d) * (size_t)d * sizeof(float) : 0;
+    const int64_t groups = norm_sizes_ok(rows, d) ? norm_groups(rows, d) : 0;
+    return groups > 1 ? (size_t)groups * (size_t)d * sizeof(float) : 0;
 }
 
 mlmc_status mlmc_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t d, int dtype, const float* weight, float eps,
@@ -392,16 +400,18 @@ mlmc_status mlmc_rms_norm_backward(const void* dy, int64_t lddy, const void* s, 
     if (dweight && (!entry_dtype_ok(grad_dtype) || !entry_ptr_ok(dweight, grad_dtype))) return MLMC_EINVAL;
     if (rows > 0 && (!entry_ptr_ok(dy, dtype) || !entry_ptr_ok(s, dtype) || !entry_ptr_ok(dx, dtype) || !rstd || !f32_ptr_ok(rstd) || !f32_ptr_ok(weight))) return MLMC_EINVAL;
     if (rows > 0 && residual && !entry_ptr_ok(residual, dtype)) return MLMC_EINVAL;
-    if (dweight && rows > 0 && (!ws || (uintptr_t)ws % 256 || ws_bytes < mlmc_rms_norm_workspace(rows, d))) return MLMC_EINVAL;
+    const size_t need = dweight ? mlmc_rms_norm_workspace(rows, d) : 0;
+    if (need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     RmsArgs a = {};
     a.dy = dy; a.lddy = lddy; a.x = s; a.ldx = lds; a.rows = rows; a.d = d; a.weight = weight; a.rstd_in = rstd; a.residual = residual; a.ldr = ldr;
-    a.dx = dx; a.lddx = lddx; a.part = dweight ? (float*)ws : nullptr; a.groups = norm_groups(rows, d);
+    a.dx = dx; a.lddx = lddx; a.part = need ? (float*)ws : nullptr; a.groups = norm_groups(rows, d); a.dweight = dweight; a.grad_dtype = grad_dtype;
     if (rows > 0) {
         const mlmc_status rc = dtype == MLMC_F32 ? rms_backward<MLMC_F32>(a, st) : rms_backward<MLMC_BF16>(a, st);
         if (rc != MLMC_OK) return rc;
     }
-    return dweight ? join_columns({a.part, rows > 0 ? a.groups : 0, d, 0, 1, {dweight, nullptr}, grad_dtype}, st) : MLMC_OK;
+    if (!dweight || (rows > 0 && !need)) return MLMC_OK;
+    return join_columns({a.part, rows > 0 ? a.groups : 0, d, 0, 1, {dweight, nullptr}, grad_dtype}, st);
 }
 
 mlmc_status mlmc_quantize(const void* x, int64_t ldx, int64_t rows, int64_t d, int dtype, uint8_t* q, int64_t ldq, float* scale, void* hip_stream) {

@@ -61,7 +61,7 @@ def logprobs_backward(**k):
     (rms, dict(rstd=A + 2)), (rms, dict(q=A, ldq=8, scale=A + 1)), (rms, dict(res=A + 2, ldr=8)),
     (rms_backward, dict(rstd=None)), (rms_backward, dict(dx=None)), (rms_backward, dict(lddx=7)), (rms_backward, dict(lddy=7)), (rms_backward, dict(lds=7)),
     (rms_backward, dict(res=A, ldr=7)), (rms_backward, dict(res=A + 1, ldr=8)), (rms_backward, dict(gd=2)), (rms_backward, dict(dw=A + 2)), (rms_backward, dict(gd=1, dw=A + 1)),
-    (rms_backward, dict(ws=None)), (rms_backward, dict(ws=A + 64)), (rms_backward, dict(wsb=8)), (rms_backward, dict(s=None)),
+    (rms_backward, dict(rows=200, ws=None)), (rms_backward, dict(rows=200, ws=A + 64)), (rms_backward, dict(rows=200, wsb=8)), (rms_backward, dict(s=None)),
     (quantize, dict(rows=-1)), (quantize, dict(d=0)), (quantize, dict(ldx=7)), (quantize, dict(ldq=7)), (quantize, dict(dtype=2)), (quantize, dict(q=None)), (quantize, dict(scale=None)),
     (quantize, dict(x=A + 2)), (quantize, dict(scale=A + 2)),
     (linear, dict(rows=-1)), (linear, dict(m=0)), (linear, dict(k=0)), (linear, dict(k=(1 << 21) + 1, ldx=1 << 22, ldw=1 << 22)), (linear, dict(ldx=7)), (linear, dict(ldw=7)),

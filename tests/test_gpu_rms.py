@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2507_05508_amd as P
+from gpu_util import launched
 from oracle import worker as O
 from test_gpu_worker import DT, U, UO, f64, near, out_like, rows, untouched, vec
 
@@ -102,6 +103,14 @@ def test_rms_norm_backward(n, d, pad, shift, dtype, grad_dtype):
         again = torch.empty_like(dw)
         P.mlmc_rms_norm_backward(t[0], t[1], w, rstd, again[1:d + 1], residual=t[2], dx=t[k])
         assert torch.equal(t[k], dx) and torch.equal(again[1:d + 1], dw[1:d + 1])
+
+
+def test_few_rows_need_no_second_launch():
+    """What one workgroup has is written by it; more leave partial sums that are joined."""
+    for n, d, more in ((16, 300, set()), (17, 300, {"k_norm_join"}), (1, 9000, set()), (1, 20000, {"k_rms_columns"}), (2, 20000, {"k_rms_columns", "k_norm_join"})):
+        s, dw = torch.ones((n, d), device="cuda"), torch.zeros(d, device="cuda")
+        assert launched(lambda: P.mlmc_rms_norm_backward(s, s, None, s[:, 0].contiguous(), dw)) == {"k_rms_backward"} | more
+        assert (P.mlmc_rms_norm_workspace(n, d) == 0) == ("k_norm_join" not in more) and bool((dw == n).all())
 
 
 def test_rms_norm_without_rows_weight_or_residual():
