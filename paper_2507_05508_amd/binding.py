@@ -586,11 +586,14 @@ class TokenLogprobs(NamedTuple):
 _E4M3 = torch.float8_e4m3fn
 
 
-def _eight_bits(n: int, d: int, like: torch.Tensor) -> torch.Tensor:
-    """A matrix of 8 bits whose rows begin at multiples of 16 bytes, which the product of such matrices reads fastest."""
+def _eight_bits(n: int, d: int, like: torch.Tensor):
+    """A matrix of 8 bits whose rows begin at multiples of 16 bytes, which the product of such matrices reads fastest, and its row distance."""
     ld = (d + 15) // 16 * 16
-    q = torch.empty((n, ld), dtype=_E4M3, device=like.device)
-    return q if ld == d else q[:, :d]
+    return torch.empty_strided((n, d), (ld, 1), dtype=_E4M3, device=like.device), ld
+
+
+def _same(x: torch.Tensor, n: int, d: int) -> torch.Tensor:
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty((n, d))     # the former takes less time
 
 
 def _or_none(t: Optional[torch.Tensor], name: str, dtype, n: int, d: int):
@@ -627,7 +630,7 @@ def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
     if residual is not None:
         p_r, ldr = residual.data_ptr(), _matrix(residual, "residual", dtype, n, d)
         if sum is None:
-            sum, lds = x.new_empty((n, d)), d
+            sum, lds = _same(x, n, d), d
         else:
             lds = _matrix(sum, "sum", dtype, n, d)
         p_s = sum.data_ptr()
@@ -636,12 +639,14 @@ def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
     if y is not None:
         p_y, ldy = y.data_ptr(), _matrix(y, "y", dtype, n, d)
     elif with_y:
-        y, ldy = x.new_empty((n, d)), d
+        y, ldy = _same(x, n, d), d
         p_y = y.data_ptr()
     if q is not None or with_q:
         if q is None:
-            q = _eight_bits(n, d, x)
-        p_q, ldq = q.data_ptr(), _matrix(q, "q", _E4M3, n, d)
+            q, ldq = _eight_bits(n, d, x)
+        else:
+            ldq = _matrix(q, "q", _E4M3, n, d)
+        p_q = q.data_ptr()
         if scale is None:
             scale = torch.empty(n, dtype=torch.float32, device=x.device)
             p_scale = scale.data_ptr()
@@ -695,10 +700,15 @@ def mlmc_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Opti
     ldx = _matrix(x, "x")
     n, d = x.shape
     if q is None:
-        q = _eight_bits(n, d, x)
+        q, ldq = _eight_bits(n, d, x)
+    else:
+        ldq = _matrix(q, "q", _E4M3, n, d)
     if scale is None:
         scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    rc = lib().mlmc_quantize(x.data_ptr(), ldx, n, d, _DTYPE[x.dtype], q.data_ptr(), _matrix(q, "q", _E4M3, n, d), _vector(scale, "scale", n), _stream())
+        p_scale = scale.data_ptr()
+    else:
+        p_scale = _vector(scale, "scale", n)
+    rc = lib().mlmc_quantize(x.data_ptr(), ldx, n, d, _DTYPE[x.dtype], q.data_ptr(), ldq, p_scale, _stream())
     if rc:
         _check(rc, "mlmc_quantize")
     return q, scale
@@ -735,7 +745,7 @@ def mlmc_dropout(x: torch.Tensor, p: float, seed: int, step: int, stream: int = 
     dtype = x.dtype
     n, d = x.shape
     if y is None:
-        y, ldy = x.new_empty((n, d)), d
+        y, ldy = _same(x, n, d), d
     else:
         ldy = _matrix(y, "y", dtype, n, d)
     if not (0 <= step < 1 << 32 and 0 <= stream < 1 << 32 and 0 <= row0 <= 1 << 32):
@@ -758,7 +768,7 @@ def mlmc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = N
     given, p_t, logprob = 0, None, None
     if tokens is not None:
         given = _given(tokens)
-        p_t = _table(tokens if tokens.dim() == 2 else tokens.unsqueeze(1), "tokens", n, given, torch.int32)
+        p_t = _answers(tokens, "tokens", n, torch.int32)
         logprob = torch.empty(tokens.shape, dtype=torch.float32, device=at)
     entropy = torch.empty(n, dtype=torch.float32, device=at) if with_entropy else None
     stats = torch.empty((n, 3), dtype=torch.float32, device=at) if with_stats else None
@@ -782,6 +792,13 @@ def _given(tokens: torch.Tensor) -> int:
     return tokens.shape[1] if tokens.dim() == 2 else 1
 
 
+def _answers(t: torch.Tensor, name: str, n: int, dtype):
+    """Address of a table with a row for each row of the logits, [n] or [n, given]."""
+    if t.dtype is not dtype or t.shape[0] != n or not t.is_contiguous() or _elsewhere(t):
+        raise MlmcError(f"{name} must be a contiguous tensor of {dtype}, [{n}] or [{n}, given], on the current CUDA device")
+    return t.data_ptr()
+
+
 def mlmc_token_logprobs_backward(logits: torch.Tensor, stats: torch.Tensor, tokens: Optional[torch.Tensor] = None, dlogprob: Optional[torch.Tensor] = None,
                                  top_idx: Optional[torch.Tensor] = None, dtop: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None,
                                  temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -798,8 +815,7 @@ def mlmc_token_logprobs_backward(logits: torch.Tensor, stats: torch.Tensor, toke
         given = _given(tokens)
         if dlogprob.shape != tokens.shape:
             raise MlmcError("dlogprob has the size of tokens")
-        p_t = _table(tokens if tokens.dim() == 2 else tokens.unsqueeze(1), "tokens", n, given, torch.int32)
-        p_g = _table(dlogprob if dlogprob.dim() == 2 else dlogprob.unsqueeze(1), "dlogprob", n, given, torch.float32)
+        p_t, p_g = _answers(tokens, "tokens", n, torch.int32), _answers(dlogprob, "dlogprob", n, torch.float32)
     if top_idx is not None:
         if top_idx.dim() != 2:
             raise MlmcError("top_idx must be a matrix")
