@@ -378,7 +378,7 @@ mlmc_status mlmc_distill(const void *logits, int64_t ldl, int64_t rows, int64_t 
  *   x: dev [rows][ldx];  residual: dev [rows][ldr] or NULL (s = x);  weight: dev [d] fp32 or NULL (1);  eps >= 0;
  *   sum: dev [rows][lds] (out) or NULL: receives s; only with a residual;  y: dev [rows][ldy] (out) or NULL;
  *   q, scale: dev [rows][ldq] bytes and [rows] fp32 (out), or both NULL: y in 8 bits as mlmc_quantize has it;  at least one of y and q;
- *   rstd: dev [rows] fp32 (out) or NULL: r, for the backward pass.  sum and y may each be x or the residual (not both the same).
+ *   rstd: dev [rows] fp32 (out) or NULL: r, for the backward pass.  sum and y may each be x or the residual, but not both the same matrix.
  * The sum of the squares is fp32: of rows for which it is infinite r is 0, and y the product with that.
  */
 mlmc_status mlmc_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int64_t rows, int64_t d, int dtype, const float *weight, float eps,
@@ -398,7 +398,7 @@ mlmc_status mlmc_rms_norm_backward(const void *dy, int64_t lddy, const void *s, 
 
 /*
  * Rows in 8 bits (e4m3: sign, 4 exponent bits of bias 7, 3 bits behind the point, greatest value 448, one NaN and no infinity):
- * scale = max_j |x_j| / 448, at least 2^-100; q_j = the e4m3 value nearest to x_j / scale, ties to even.  q_j stands for q_j scale.
+ * scale = max_j |x_j| / 448, at least 2^-100; q_j = the e4m3 value nearest to x_j / scale, ties to even (both quotients in fp32).  q_j stands for q_j scale.
  *   x: dev [rows][ldx];  q: dev [rows][ldq] bytes (out);  scale: dev [rows] fp32 (out).
  *   A row that holds a NaN or an infinity has the scale NaN and nothing but NaN.
  */

@@ -57,7 +57,7 @@ static const char* const k_names[K_NUM] = {
     "k_rs_hist", "k_rs_scan", "k_rs_scatter", "k_sb_norms", "k_sb_draw", "k_sb_mark", "k_sb_offsets", "k_sb_write", "k_se_count", "k_se_scan",
     "k_se_split", "k_se_zone", "k_row_select", "k_row_write", "k_c16_hist", "k_c16_reduce", "k_c16_scan", "k_c16_mark", "k_c16_offsets", "k_c16_write",
     "k_bits_extract_words", "k_agg_words", "k_scan_marks", "k_norm_forward", "k_norm_backward", "k_norm_columns", "k_norm_join", "k_linear", "k_linear_few", "k_linear_join", "k_linear_pack", "k_distill", "k_distill_stats",
-    "k_rms_forward", "k_rms_backward", "k_rms_columns", "k_quantize", "k_linear_q8", "k_linear_q8_few", "k_dropout", "k_logprobs", "k_logprobs_rows", "k_logprobs_backward"};
+    "k_rms_forward", "k_rms_backward", "k_rms_columns", "k_quantize", "k_linear_q8", "k_linear_q8_tile", "k_linear_q8_few", "k_dropout", "k_logprobs", "k_logprobs_rows", "k_logprobs_backward"};
 struct ProfPair { int id; hipEvent_t e0, e1; };
 static std::vector<ProfPair> g_pending;
 static std::vector<ProfPair> g_free;

@@ -299,7 +299,7 @@ enum KernelId {
     K_ROW_SELECT, K_ROW_WRITE, K_C16_HIST, K_C16_REDUCE, K_C16_SCAN, K_C16_MARK, K_C16_OFFSETS, K_C16_WRITE,
     K_BITS_WORDS, K_AGG_WORDS, K_SCAN_MARKS,
     K_NORM_FORWARD, K_NORM_BACKWARD, K_NORM_COLUMNS, K_NORM_JOIN, K_LINEAR, K_LINEAR_FEW, K_LINEAR_JOIN, K_LINEAR_PACK, K_DISTILL, K_DISTILL_STATS,
-    K_RMS_FORWARD, K_RMS_BACKWARD, K_RMS_COLUMNS, K_QUANTIZE, K_LINEAR_Q8, K_LINEAR_Q8_FEW, K_DROPOUT, K_LOGPROBS, K_LOGPROBS_ROWS, K_LOGPROBS_BACKWARD, K_NUM
+    K_RMS_FORWARD, K_RMS_BACKWARD, K_RMS_COLUMNS, K_QUANTIZE, K_LINEAR_Q8, K_LINEAR_Q8_TILE, K_LINEAR_Q8_FEW, K_DROPOUT, K_LOGPROBS, K_LOGPROBS_ROWS, K_LOGPROBS_BACKWARD, K_NUM
 };
 extern bool g_prof_on;
 void prof_begin(int id, hipStream_t st);

@@ -687,8 +687,8 @@ enum LinearTile { TILE_32 = 0, TILE_64, TILE_128, TILE_256, TILES };
 struct TileCost { int rows, cols; float alone_us[2], among_us[2], round_us; };   // [dtype]
 constexpr TileCost tile_costs[TILES] = {{32, 128, {0.55f, 0.42f}, {0.53f, 0.28f}, 0.7f}, {64, 128, {0.95f, 0.44f}, {0.95f, 0.33f}, 1.3f},
                                         {128, 128, {1.85f, 0.70f}, {1.85f, 0.50f}, 2.5f}, {256, 256, {0.f, 1.50f}, {0.f, 1.60f}, 11.f}};
-// The large tile of 8 bits has its results stored by one wave a SIMD: 8192 x 4096 x 1024 62 us, by tiles of 128 54; 8192 x 8192 x 2048 158 and 162; 16384 x 1024 x 1024 28 and 29; 4096 x 4096 x 4096 65 and 69.
-constexpr float Q8_BIG_ROUND_US = 15.f;
+// The large tile of 8 bits: 8192 x 4096 x 4096 107 us, 4096 x 4096 x 4096 56, by tiles of 128 159 and 69.
+constexpr TileCost q8_big_cost = {256, 256, {0.f, 1.35f}, {0.f, 1.35f}, 9.f};
 constexpr float LAUNCH_US = 5.f, JOIN_US = 3.f, JOIN_ENTRY_US = 1.6e-6f;
 constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
 
@@ -704,12 +704,12 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
     float least = 3.0e38f;
     for (int t = 0; t < TILES; ++t) {
         if (t == TILE_256 && (dtype == MLMC_F32 || !fast)) continue;
-        const TileCost& k = tile_costs[t];
+        const TileCost& k = dtype == DT_E4M3 && t == TILE_256 ? q8_big_cost : tile_costs[t];
         const int64_t tiles = ((I + k.rows - 1) / k.rows) * ((J + k.cols - 1) / k.cols);
         for (int s = 1; s <= (dtype == DT_E4M3 && t == TILE_256 ? 1 : SPLITS_MAX) && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
             const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
             if (parts != s) continue;
-            const float us = LAUNCH_US + (float)rounds * ((dtype == DT_E4M3 && t == TILE_256 ? Q8_BIG_ROUND_US : k.round_us) + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
+            const float us = LAUNCH_US + (float)rounds * (k.round_us + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
                              (s > 1 ? JOIN_US + JOIN_ENTRY_US * (float)(s * I) * (float)J : 0.f);
             if (us < least) {
                 least = us;
@@ -737,7 +737,7 @@ template <int DT, int WM, int WN, int FM, int FN, bool AA, bool BA, int WAY> sta
     g.tiles_i = (int)((g.I + TM - 1) / TM);
     g.tiles_j = (int)((g.J + TN - 1) / TN);
     const unsigned grid = (unsigned)((int64_t)g.tiles_i * g.tiles_j * g.splits);
-    MLMC_LAUNCH(DT == DT_E4M3 ? K_LINEAR_Q8 : K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, WAY><<<grid, WM * WN * 64, 0, st>>>(g)));
+    MLMC_LAUNCH(DT == DT_E4M3 ? K_LINEAR_Q8_TILE : K_LINEAR, st, (k_linear_tile<DT, WM, WN, FM, FN, AA, BA, WAY><<<grid, WM * WN * 64, 0, st>>>(g)));
     if (g.splits > 1) {
         const unsigned groups = (unsigned)((g.I * ((g.J + 7) / 8) + g.I + 255) / 256);
         MLMC_LAUNCH(K_LINEAR_JOIN, st, (k_linear_join<DT><<<groups, 256, 0, st>>>(g)));

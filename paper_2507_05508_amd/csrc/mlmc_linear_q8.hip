@@ -10,12 +10,37 @@ namespace mlmc {
 
 // The large tile of matrices whose rows are aligned: 256 x 256 by 4 waves of 128 x 128, a workgroup for every CU with tile after tile, the first loads of the next one ahead of the stores of the last.
 // Loads and barriers as in k_linear_tile; a wave's fragments of the next half step are read over those of this one, A's as soon as its instructions have gone out.
-// 8192 x 4096 x 4096: by 8 waves of 128 x 64 (k_linear_tile) 148 us; by two workgroups a CU, 128 x 256 each and steps of 64 bytes, 186: the matrix units take 1.55 us a step at the clock that
-// they leave the card, and half as much again from the L2 makes that 2.5.
+// 8192 x 4096 x 4096: 107 us (2.57 PFLOP/s; a library product without the epilogue 89 to 98), with gelu 121; by 8 waves of 128 x 64 (k_linear_tile) 20 more; by two workgroups a CU, 128 x 256 each and
+// steps of 64 bytes, 45 more: half as much again comes from the L2.
 constexpr int BIG = 256, BIG_T = 256, BIG_F = 4;   // (a thread for every row of the tile)
 using v2b = __bf16 __attribute__((ext_vector_type(2)));
 using v4b = __bf16 __attribute__((ext_vector_type(4)));
 using v4b_u = __bf16 __attribute__((ext_vector_type(4), aligned(2)));   // at any entry's place
+
+// Chunk k of lane l of four becomes chunk l of lane k.
+__device__ inline void transpose_fours(chunk_t (&c)[4], int lane) {
+    const auto from = [](int v, auto ctrl) { return __builtin_amdgcn_update_dpp(v, v, decltype(ctrl)::value, 0xF, 0xF, false); };
+    constexpr std::integral_constant<int, 0xB1> next;   // lanes 2k and 2k + 1
+    constexpr std::integral_constant<int, 0x4E> pair;   // the pairs of four
+    const bool one = lane & 1, two = lane & 2;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        int v[4] = {c[0][d], c[1][d], c[2][d], c[3][d]}, u[4];
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            const int a = from(v[k], next), b = from(v[k + 1], next);   // by all lanes, ahead of the choice
+            u[k] = one ? b : v[k];
+            u[k + 1] = one ? v[k + 1] : a;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int a = from(u[k], pair), b = from(u[k + 2], pair);
+            c[k][d] = two ? b : u[k];
+            c[k + 2][d] = two ? u[k + 2] : a;
+        }
+    }
+}
+
 __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
     using Op = Operand<DT_E4M3, true, BIG, BIG_T, WAY_CHUNKS>;
     constexpr int STEP = Op::STEP, F = BIG_F;
@@ -42,13 +67,20 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         B.init(g.b, g.ldb, j0, g.J, g.C, thread);
     };
     v16f acc[F][F];
-    Fragments<DT_E4M3, true, BIG, F> FA, FB;
+    Fragments<DT_E4M3, true, BIG, F> FA;
     FA.init(wm * F);
-    FB.init(wn * F);
+    // B's fragments in pairs, of 64 columns: n even has columns 0 to 15 and 32 to 47, n odd the others, so that in the end a lane's results of a pair are 32 neighbouring ones
+    int place_b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) place_b[k] = Op::L::slot(wn * 128 + (lane & 16) * 2 + (lane & 15), k * 2 + half);
+    const auto fragment_b = [&](const chunk_t* s, int n, int q) {
+        const int at = ((n >> 1) * 64 + (n & 1) * 16) * 8;
+        return __builtin_shufflevector(s[place_b[2 * q] + at], s[place_b[2 * q + 1] + at], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     v8i fa[F], fb[2][F];
     const auto read = [&](const chunk_t* sa, const chunk_t* sb) {
 #pragma unroll
-        for (int n = 0; n < F; ++n) fb[0][n] = FB.get(sb, n, 0);
+        for (int n = 0; n < F; ++n) fb[0][n] = fragment_b(sb, n, 0);
 #pragma unroll
         for (int m = 0; m < F; ++m) fa[m] = FA.get(sa, m, 0);
     };
@@ -57,7 +89,7 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         constexpr bool MORE = decltype(more)::value;
 #pragma unroll
         for (int n = 0; n < F; ++n)
-            if (MORE) fb[1 - q][n] = FB.get(sb, n, 1 - q);
+            if (MORE) fb[1 - q][n] = fragment_b(sb, n, 1 - q);
 #pragma unroll
         for (int m = 0; m < F; ++m) {
 #pragma unroll
@@ -129,7 +161,7 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
             multiply_half(1, std::false_type{}, a0, b0);
             arrived();
         }
-        const int64_t oi = i0 + wm * 128 + (lane & 31), oj = j0 + wn * 128;
+        const int64_t i0_done = i0, oi = i0 + wm * 128 + (lane & 31), oj = j0 + wn * 128;
         float rs[F];   // ahead of the next tile's loads: what is waited for comes in order
 #pragma unroll
         for (int m = 0; m < F; ++m) rs[m] = g.row_scale[min(oi + m * 32, g.I - 1)];
@@ -140,39 +172,37 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
             A.fetch(a0, 0, c_whole);
             B.fetch(b0, 0, c_whole);
         }
-        // A lane has four neighbouring entries of a row in four registers (the operands are exchanged): rounded and exchanged between the halves of the wave they are eight, 16 bytes.  (By way of the
-        // second buffers, 256 bytes of each of four rows a store, the waits of the one wave a SIMD took more than the fuller lines gave: 154 us instead of 139.)
+        // A lane has four neighbouring entries of a row in four registers (the operands are exchanged).  Rounded and exchanged between the halves of the wave they are 64 bytes of a pair of fragments,
+        // and transposed among four lanes, 16 bytes each of the 64 of one row: a store has whole sectors of 16 rows.  (16 bytes of each of 64 places a store: 126 us instead of 115, and twice
+        // the bytes written to HBM; by way of LDS the waits of the one wave a SIMD took more than that gave.)
         const auto results = [&](auto act, auto whole) __attribute__((always_inline)) {
             constexpr int ACT = decltype(act)::value;
             constexpr bool WHOLE = decltype(whole)::value;   // all columns of the tile
+            const int64_t is = i0_done + wm * 128 + (lane & 28), js = oj + half * 32 + (lane & 3) * 8;
+            __bf16* const y = (__bf16*)g.out + is * g.ldo + js;
 #pragma unroll
-            for (int n = 0; n < F; ++n)
+            for (int p = 0; p < F / 2; ++p)
 #pragma unroll
-                for (int q = 0; q < 4; q += 2) {
-                    v4f cs[2], bs[2];
+                for (int m = 0; m < F; ++m) {
+                    __builtin_amdgcn_sched_barrier(0);   // one after the other: there are no registers for more
+                    chunk_t out[4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int at = wn * 128 + n * 32 + (q + h) * 8 + half * 4;
-                        cs[h] = *(const v4f*)(scales + at);
-                        bs[h] = *(const v4f*)(biases + at);
-                    }
-                    const int64_t j = oj + n * 32 + (q + half) * 8;   // of the eight that the lane stores
+                    for (int k = 0; k < 2; ++k) {
+                        const int n = 2 * p + k;
+                        unsigned packed[4][2];
 #pragma unroll
-                    for (int m = 0; m < F; ++m) {
-                        const int64_t i = oi + m * 32;
-                        unsigned packed[2][2];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                        for (int q = 0; q < 4; ++q) {
+                            const int col = p * 64 + (q >> 1) * 32 + k * 16 + (q & 1) * 8 + half * 4;
+                            const v4f cs = *(const v4f*)(scales + wn * 128 + col), bs = *(const v4f*)(biases + wn * 128 + col);
                             float v[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                v[e] = fmaf(acc[m][n][(q + h) * 4 + e] * rs[m], cs[h][e], bs[h][e]);
+                                v[e] = fmaf(acc[m][n][q * 4 + e] * rs[m], cs[e], bs[e]);
                                 if (ACT == MLMC_ACT_GELU) v[e] = gelu<MLMC_BF16>(v[e]);
                                 if (ACT == MLMC_ACT_RELU) v[e] = relu(v[e]);
                             }
                             if (g.residual) {
-                                const int64_t jr = oj + n * 32 + (q + h) * 8 + half * 4;
-                                const __bf16* r = (const __bf16*)g.residual + min(i, g.I - 1) * g.ldr + jr;
+                                const __bf16* r = (const __bf16*)g.residual + min(oi + m * 32, g.I - 1) * g.ldr + oj + col;
                                 if (WHOLE) {
                                     const v4b u = *(const v4b_u*)r;
 #pragma unroll
@@ -180,27 +210,32 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
                                 } else {
 #pragma unroll
                                     for (int e = 0; e < 4; ++e)
-                                        if (jr + e < g.J) v[e] += (float)r[e];
+                                        if (oj + col + e < g.J) v[e] += (float)r[e];
                                 }
                             }
 #pragma unroll
-                            for (int w = 0; w < 2; ++w) packed[h][w] = __builtin_bit_cast(unsigned, v2b{(__bf16)v[2 * w], (__bf16)v[2 * w + 1]});
+                            for (int w = 0; w < 2; ++w) packed[q][w] = __builtin_bit_cast(unsigned, v2b{(__bf16)v[2 * w], (__bf16)v[2 * w + 1]});
                         }
-                        chunk_t out;
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {   // lanes 0 to 31 get the first eight, the others the second
-                            const auto both = __builtin_amdgcn_permlane32_swap(packed[0][w], packed[1][w], false, false);
-                            out[w] = (int)both[0];
-                            out[2 + w] = (int)both[1];
-                        }
-                        if (i >= g.I) continue;
-                        __bf16* y = (__bf16*)g.out + i * g.ldo + j;
-                        if (WHOLE) *(chunk_u*)y = out;
+                        for (int h = 0; h < 2; ++h)   // lanes 0 to 31 get the first sixteen columns, the others the second
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) {
+                                const auto both = __builtin_amdgcn_permlane32_swap(packed[h][w], packed[2 + h][w], false, false);
+                                out[2 * k + h][w] = (int)both[0];
+                                out[2 * k + h][2 + w] = (int)both[1];
+                            }
+                    }
+                    transpose_fours(out, lane);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (is + m * 32 + r >= g.I) continue;
+                        __bf16* to = y + (m * 32 + r) * g.ldo + p * 64;
+                        if (WHOLE) *(chunk_u*)to = out[r];
                         else {
-                            const v8b u = __builtin_bit_cast(v8b, out);
+                            const v8b u = __builtin_bit_cast(v8b, out[r]);
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                if (j + e < g.J) y[e] = u[e];
+                                if (js + p * 64 + e < g.J) to[e] = u[e];
                         }
                     }
                 }

@@ -388,7 +388,7 @@ mlmc_status mlmc_rms_norm(const void* x, int64_t ldx, const void* residual, int6
     if ((sum && (!residual || lds < d)) || (y && ldy < d) || (q && ldq < d)) return MLMC_EINVAL;
     if (rows == 0) return MLMC_OK;
     if (!entry_ptr_ok(x, dtype) || (residual && !entry_ptr_ok(residual, dtype)) || (sum && !entry_ptr_ok(sum, dtype)) || (y && !entry_ptr_ok(y, dtype))) return MLMC_EINVAL;
-    if ((!y && !q) || (q && !scale) || !f32_ptr_ok(weight) || !f32_ptr_ok(scale) || !f32_ptr_ok(rstd)) return MLMC_EINVAL;
+    if ((!y && !q) || (y && y == sum) || (q && !scale) || !f32_ptr_ok(weight) || !f32_ptr_ok(scale) || !f32_ptr_ok(rstd)) return MLMC_EINVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     RmsArgs a = {};
     a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.rows = rows; a.d = d; a.weight = weight; a.eps = eps;

@@ -58,7 +58,7 @@ def logprobs_backward(**k):
     (rms, dict(rows=-1)), (rms, dict(rows=1 << 31)), (rms, dict(d=0)), (rms, dict(dtype=2)), (rms, dict(ldx=7)), (rms, dict(ldy=7)), (rms, dict(res=A, ldr=7)),
     (rms, dict(sum=A, lds=8)), (rms, dict(res=A, ldr=8, sum=A, lds=7)), (rms, dict(eps=-1.0)), (rms, dict(eps=NAN)), (rms, dict(eps=INF)), (rms, dict(y=None)),
     (rms, dict(q=A, ldq=8)), (rms, dict(q=A, ldq=7, scale=A)), (rms, dict(x=None)), (rms, dict(x=A + 2)), (rms, dict(dtype=1, x=A + 1)), (rms, dict(weight=A + 1)),
-    (rms, dict(rstd=A + 2)), (rms, dict(q=A, ldq=8, scale=A + 1)), (rms, dict(res=A + 2, ldr=8)),
+    (rms, dict(rstd=A + 2)), (rms, dict(res=A, ldr=8, sum=A, lds=8, y=A)), (rms, dict(q=A, ldq=8, scale=A + 1)), (rms, dict(res=A + 2, ldr=8)),
     (rms_backward, dict(rstd=None)), (rms_backward, dict(dx=None)), (rms_backward, dict(lddx=7)), (rms_backward, dict(lddy=7)), (rms_backward, dict(lds=7)),
     (rms_backward, dict(res=A, ldr=7)), (rms_backward, dict(res=A + 1, ldr=8)), (rms_backward, dict(gd=2)), (rms_backward, dict(dw=A + 2)), (rms_backward, dict(gd=1, dw=A + 1)),
     (rms_backward, dict(rows=200, ws=None)), (rms_backward, dict(rows=200, ws=A + 64)), (rms_backward, dict(rows=200, wsb=8)), (rms_backward, dict(s=None)),

@@ -18,7 +18,10 @@ SIZES = [  # rows, outputs, inputs, pad, shift
     (1, 1, 1, 0, 0), (1, 3, 5, 1, 1), (2, 17, 15, 0, 0), (3, 16, 16, 0, 0), (5, 33, 64, 0, 0), (1, 128, 257, 0, 0), (16, 100, 1000, 8, 0), (16, 4096, 4096, 0, 0), (1, 4096, 4096, 0, 0),
     (17, 64, 128, 0, 0), (33, 65, 127, 1, 3), (40, 129, 130, 0, 0), (64, 128, 512, 0, 0), (100, 200, 300, 5, 0), (129, 257, 1023, 0, 0), (255, 256, 1024, 16, 16), (256, 512, 8192, 0, 0),
     (300, 1000, 13, 0, 0), (513, 1025, 2049, 0, 0), (1000, 640, 4096, 0, 4), (2048, 2048, 1024, 0, 0), (2049, 2305, 1025, 3, 1), (4096, 4096, 512, 0, 0), (4100, 4000, 640, 0, 0), (37, 8192, 96, 0, 0),
-    (4000, 4001, 1072, 0, 0), (4000, 4001, 1071, 1, 0), (3000, 4100, 513, 15, 0), (8200, 2050, 127, 1, 0), (4000, 4000, 112, 16, 0),   # the large tile with what a step of 128 leaves over
+    (4000, 4001, 1072, 0, 0), (4000, 4001, 1071, 1, 0), (3000, 4100, 513, 15, 0), (8200, 2050, 127, 1, 0), (4000, 4000, 112, 16, 0), (3841, 4097, 4224, 16, 0),
+]
+BIG = [  # the large tile: whole tiles, more of them than CUs, rows and columns cut, what a step of 128 leaves over, rows at any place (copied to aligned ones)
+    (4096, 4096, 4096, 0, 0), (8192, 4096, 2048, 0, 0), (4000, 4001, 4112, 0, 0), (4000, 4002, 4111, 1, 0), (3841, 4090, 4224, 16, 0), (4003, 3850, 3999, 0, 0), (8190, 5000, 1920, 0, 0),
 ]
 
 
@@ -39,7 +42,7 @@ def powers(gen, n):
     return torch.exp2(torch.randint(-3, 4, (n,), device="cuda", generator=gen).float())
 
 
-@pytest.mark.parametrize("n,m,k,pad,shift", SIZES)
+@pytest.mark.parametrize("n,m,k,pad,shift", SIZES + BIG)
 def test_linear_q8_to_the_bit(n, m, k, pad, shift):
     print(f"linear_q8 n={n} m={m} k={k} pad={pad} shift={shift}", flush=True)
     gen = torch.Generator(device="cuda")
@@ -60,6 +63,8 @@ def test_linear_q8_to_the_bit(n, m, k, pad, shift):
             P.mlmc_linear_q8(x, xs, w, ws, bias, act=ACT[act], residual=r, y=r)
             assert torch.equal(r, y)
     assert torch.equal(P.mlmc_linear_q8(x, xs, w, ws), v.float().to(torch.bfloat16))
+    if (n, m, k, pad, shift) in BIG:
+        assert "k_linear_q8" in launched(lambda: P.mlmc_linear_q8(x, xs, w, ws))
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "gelu"])
@@ -104,7 +109,8 @@ def test_linear_q8_kernels():
         x, w = whole(gen, n, k, pad), whole(gen, m, k, pad)
         return launched(lambda: P.mlmc_linear_q8(x, torch.ones(n, device="cuda"), w, torch.ones(m, device="cuda")))
     assert run(1, 4096, 4096) == {"k_linear_q8_few"}
-    assert run(4096, 4096, 512) == {"k_linear_q8"}
+    assert run(4096, 4096, 4096) == {"k_linear_q8"}
+    assert run(100, 4096, 512) == {"k_linear_q8_tile"}
     assert "k_linear_join" in run(128, 128, 8192)
     assert "k_linear_pack" in run(4096, 4096, 1024, pad=5)
 
