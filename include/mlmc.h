@@ -398,7 +398,7 @@ mlmc_status mlmc_rms_norm_backward(const void *dy, int64_t lddy, const void *s, 
 
 /*
  * Rows in 8 bits (e4m3: sign, 4 exponent bits of bias 7, 3 bits behind the point, greatest value 448, one NaN and no infinity):
- * scale = max_j |x_j| / 448, at least 2^-100; q_j = the e4m3 value nearest to x_j / scale, ties to even (both quotients in fp32).  q_j stands for q_j scale.
+ * scale = max_j |x_j| / 448, at least 2^-100; q_j = the e4m3 value nearest to 448 x_j / max_j |x_j| (with the least scale to x_j 2^100), ties to even.  q_j stands for q_j scale.
  *   x: dev [rows][ldx];  q: dev [rows][ldq] bytes (out);  scale: dev [rows] fp32 (out).
  *   A row that holds a NaN or an infinity has the scale NaN and nothing but NaN.
  */

@@ -133,8 +133,9 @@ def quantize(x):
     """e4m3 entries and the scale of every row; rows with a NaN or an infinity are NaN."""
     most = np.abs(x).max(axis=1)
     scale = np.where(np.isfinite(x).all(axis=1), np.maximum(most / 448.0, 2.0 ** -100), np.nan)
-    with np.errstate(invalid="ignore"):
-        return e4m3(x / scale[:, None]), scale
+    with np.errstate(invalid="ignore", divide="ignore"):      # not over the scale, whose rounding would move what lies half way between two values
+        v = np.where(scale[:, None] > 2.0 ** -100, x * 448.0 / most[:, None], x * 2.0 ** 100)
+    return e4m3(np.where(np.isnan(scale[:, None]), np.nan, v)), scale
 
 
 def dropout_keep(n, d, least, seed, step, stream, row0=0):

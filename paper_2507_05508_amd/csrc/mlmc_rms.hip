@@ -1,7 +1,7 @@
 // Root-mean-square norm of rows with the residual's addition, forward and backward, and rows brought into 8 bits (entry points mlmc_rms_norm, mlmc_rms_norm_backward,
 // mlmc_quantize).
 //
-//   s = x + residual,  r = 1 / sqrt(mean_j s_j^2 + eps),  y_j = s_j r w_j;  in 8 bits: scale = max_j |y_j| / 448 (at least 2^-100), q_j = e4m3(y_j / scale)
+//   s = x + residual,  r = 1 / sqrt(mean_j s_j^2 + eps),  y_j = s_j r w_j;  in 8 bits: scale = max_j |y_j| / 448 (at least 2^-100), q_j = e4m3(448 y_j / max |y|)
 //   backward, with h_j = s_j r and c_j = dy_j w_j:  ds_j = r (c_j - h_j mean(c h)) + what reaches s by another way,  dw_j = sum_rows dy_j h_j
 //
 // 448 is the greatest e4m3 value.  One scale a row, so that a product of two such matrices takes its scales in the epilogue.  The least scale keeps the division within
@@ -33,15 +33,24 @@ struct RmsArgs {
 
 constexpr float E4M3_MAX = 448.f, LEAST_SCALE = 0x1p-100f;
 
-// the scale of a row whose greatest magnitude has these bits; NaN for infinities and NaN, which have the greatest bits
-__device__ inline float row_scale(uint32_t most) {
-    const float s = __builtin_bit_cast(float, most) / E4M3_MAX;
-    return most >= 0x7f800000u ? __builtin_nanf("") : fmaxf(s, LEAST_SCALE);
-}
-// y / scale by the reciprocal and what that leaves over: the quotient rounded to nearest, so that what lies half way between two e4m3 values goes to the even one
-__device__ inline float over_scale(float y, float scale, float inv) {
-    const float q = y * inv;
-    return fmaf(fmaf(-q, scale, y), inv, q);
+// What brings a row whose greatest magnitude has these bits into 8 bits: its scale (NaN for infinities and NaN, which have the greatest bits), and the scale's inverse 448 / greatest as a sum of
+// two, so that entries are rounded once on their way to e4m3, where they lie next to the middle of two values too.
+struct ToEight {
+    float scale, hi, lo;
+    __device__ ToEight(uint32_t most) {
+        const float m = __builtin_bit_cast(float, most);
+        scale = fmaxf(m / E4M3_MAX, LEAST_SCALE);
+        hi = m < E4M3_MAX * LEAST_SCALE ? 1.0f / LEAST_SCALE : E4M3_MAX / m;
+        lo = m < E4M3_MAX * LEAST_SCALE ? 0.f : fmaf(-hi, m, E4M3_MAX) / m;
+        if (most >= 0x7f800000u) scale = hi = __builtin_nanf("");
+    }
+    __device__ float operator()(float y, float rest) const { return fmaf(y, hi, fmaf(y, lo, rest * hi)); }   // of y + rest
+};
+// s r w, rounded once, and what that leaves over
+__device__ inline float normed(float s, float r, float w, float& rest) {
+    const float h = s * r, c = fmaf(s, r, -h) * w, y = fmaf(h, w, c);
+    rest = fmaf(h, w, -y) + c;
+    return y;
 }
 __device__ inline int four_e4m3(float a, float b, float c, float d) {
     return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
@@ -110,7 +119,7 @@ template <int DT, int T, int P> __device__ inline void store_e4m3(const RowChunk
 
 // A workgroup takes WG / T rows at a time, and the weight stays in registers from round to round.  The next round's rows are on their way while one is worked on.  NORM: else rows are
 // only brought into 8 bits.  Every row has its own threads, which read all of it before they write: outputs may lie in the inputs' place.
-template <int DT, int T, int P, int WG, bool NORM, bool RES> __global__ __launch_bounds__(WG, P <= 8 ? 8 : 4) void k_rms_forward_rows(RmsArgs a) {
+template <int DT, int T, int P, int WG, bool NORM, bool RES> __global__ __launch_bounds__(WG, !NORM && P <= 8 ? 8 : 4) void k_rms_forward_rows(RmsArgs a) {
     using Row = RowChunks<DT, T, P>;
     constexpr int R = WG / T;
     __shared__ float part[2][WG / 64];
@@ -151,22 +160,39 @@ template <int DT, int T, int P, int WG, bool NORM, bool RES> __global__ __launch
             const float rstd = inverse_root(fmaf(s, inv_d, a.eps));
             if (here && RES && a.sum) of.store((entry_t<DT>*)a.sum + row * a.lds, x);
             if (here && a.rstd && threadIdx.x % T == 0) a.rstd[row] = rstd;
+            float y[P], rest;
+            if (!a.q) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) x[e] = x[e] * rstd * w[e];
-            if (here && a.y) of.store((entry_t<DT>*)a.y + row * a.ldy, x);
-        }
-        if (!NORM || a.q) {
-            if (NORM) of.cut(x);   // zero times an infinite weight or root
+                for (int e = 0; e < P; ++e) x[e] = normed(x[e], rstd, w[e], rest);
+                if (here) of.store((entry_t<DT>*)a.y + row * a.ldy, x);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < P; ++e) y[e] = normed(x[e], rstd, w[e], rest);
+            if (here && a.y) of.store((entry_t<DT>*)a.y + row * a.ldy, y);
+            of.cut(y);   // zero times an infinite weight or root
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < P; ++e) m = max(m, magnitude(y[e]));
+            const ToEight eight(row_most<T>(m, most[odd]));
+            if (!here) continue;
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                y[e] = normed(x[e], rstd, w[e], rest);
+                y[e] = eight(y[e], rest);
+            }
+            store_e4m3(of, a.q + row * a.ldq, y);
+            if (threadIdx.x % T == 0) a.scale[row] = eight.scale;
+        } else {
             uint32_t m = 0;
 #pragma unroll
             for (int e = 0; e < P; ++e) m = max(m, magnitude(x[e]));
-            const float scale = row_scale(row_most<T>(m, most[odd])), inv = 1.0f / scale;
-            if (here) {
+            const ToEight eight(row_most<T>(m, most[odd]));
+            if (!here) continue;
 #pragma unroll
-                for (int e = 0; e < P; ++e) x[e] = over_scale(x[e], scale, inv);
-                store_e4m3(of, a.q + row * a.ldq, x);
-                if (threadIdx.x % T == 0) a.scale[row] = scale;
-            }
+            for (int e = 0; e < P; ++e) x[e] = eight(x[e], 0.f);
+            store_e4m3(of, a.q + row * a.ldq, x);
+            if (threadIdx.x % T == 0) a.scale[row] = eight.scale;
         }
     }
 }
@@ -267,7 +293,7 @@ template <int DT, bool NORM> __global__ __launch_bounds__(RMS_WG) void k_rms_for
     const entry_t<DT>* x = (const entry_t<DT>*)a.x + row * a.ldx;
     const entry_t<DT>* u = a.residual ? (const entry_t<DT>*)a.residual + row * a.ldr : nullptr;
     const auto entry = [&](int64_t j) { return u ? to_f32(x[j]) + to_f32(u[j]) : to_f32(x[j]); };
-    float rstd = 1.0f, scale = 1.0f, inv = 1.0f;
+    float rstd = 1.0f;
     if (NORM) {
         float s = 0.f;
         for (int64_t j = threadIdx.x; j < a.d; j += RMS_WG) {
@@ -276,22 +302,26 @@ template <int DT, bool NORM> __global__ __launch_bounds__(RMS_WG) void k_rms_for
         }
         rstd = inverse_root(row_sum<RMS_WG>(s, part) / (float)a.d + a.eps);
     }
-    const auto normed = [&](float v, int64_t j) { return NORM ? v * rstd * (a.weight ? a.weight[j] : 1.0f) : v; };
+    const auto result = [&](float v, int64_t j, float& rest) {
+        rest = 0.f;
+        return NORM ? normed(v, rstd, a.weight ? a.weight[j] : 1.0f, rest) : v;
+    };
+    float rest;
+    uint32_t m = 0;
     if (a.q) {
-        uint32_t m = 0;
-        for (int64_t j = threadIdx.x; j < a.d; j += RMS_WG) m = max(m, magnitude(normed(entry(j), j)));
-        scale = row_scale(row_most<RMS_WG>(m, most));
-        inv = 1.0f / scale;
+        for (int64_t j = threadIdx.x; j < a.d; j += RMS_WG) m = max(m, magnitude(result(entry(j), j, rest)));
+        m = row_most<RMS_WG>(m, most);
     }
+    const ToEight eight(m);
     for (int64_t j = threadIdx.x; j < a.d; j += RMS_WG) {
-        const float v = entry(j), y = normed(v, j);
+        const float v = entry(j), y = result(v, j, rest);
         if (u && a.sum) ((entry_t<DT>*)a.sum)[row * a.lds + j] = from_f32<DT>(v);
         if (a.y) ((entry_t<DT>*)a.y)[row * a.ldy + j] = from_f32<DT>(y);
-        if (a.q) a.q[row * a.ldq + j] = (uint8_t)four_e4m3(over_scale(y, scale, inv), 0.f, 0.f, 0.f);
+        if (a.q) a.q[row * a.ldq + j] = (uint8_t)four_e4m3(eight(y, rest), 0.f, 0.f, 0.f);
     }
     if (threadIdx.x == 0) {
         if (NORM && a.rstd) a.rstd[row] = rstd;
-        if (a.q) a.scale[row] = scale;
+        if (a.q) a.scale[row] = eight.scale;
     }
 }
 
