@@ -107,7 +107,7 @@ using namespace mlmc;
 extern "C" mlmc_status mlmc_dropout(const void* x, int64_t ldx, int64_t rows, int64_t d, int dtype, double p, uint64_t seed, uint64_t step, uint32_t stream, int64_t row0,
                                     const void* residual, int64_t ldr, void* y, int64_t ldy, void* hip_stream) {
     if (rows < 0 || rows >= ((int64_t)1 << 31) || d < 1 || d >= ((int64_t)1 << 31) || !entry_dtype_ok(dtype) || ldx < d || ldy < d || (residual && ldr < d)) return MLMC_EINVAL;
-    if (!(p >= 0.0) || !(p * 65536.0 + 0.5 < 65536.0) || step >> 32 || row0 < 0 || row0 + rows > ((int64_t)1 << 32) || row0 > ((int64_t)1 << 32)) return MLMC_EINVAL;
+    if (!(p >= 0.0) || !(p * 65536.0 + 0.5 < 65536.0) || step >> 32 || row0 < 0 || row0 > ((int64_t)1 << 32) - rows) return MLMC_EINVAL;
     if (rows == 0) return MLMC_OK;
     if (!entry_ptr_ok(x, dtype) || !entry_ptr_ok(y, dtype) || (residual && !entry_ptr_ok(residual, dtype))) return MLMC_EINVAL;
     DropoutArgs a = {};

@@ -455,6 +455,7 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
             n = number;
         }
         if (n > ROOM) {
+            __syncthreads();   // all waves have read the number
             if (wave == 0) {
                 n = top_by_bisection<DT>(a, s, groups, found, list);
                 if (lane == 0) number = n;
