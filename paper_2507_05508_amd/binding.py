@@ -377,7 +377,8 @@ def _matrix(t: torch.Tensor, name: str, dtype=None, n: int = -1, d: int = -1) ->
         raise MlmcError(f"{name} must be a matrix") from None
     if (t.dtype is not dtype and (dtype is not None or t.dtype not in _DTYPE)) or (n >= 0 and rows != n) or (d >= 0 and cols != d):
         raise MlmcError(f"{name} must be of " + ("float32 or bfloat16" if dtype is None else str(dtype)) + f" and have the size that the others give it (it is {rows} x {cols})")
-    if _elsewhere(t):
+    at = t.get_device()
+    if at < 0 or at != torch._C._cuda_getDevice():     # _elsewhere, without the call
         raise MlmcError(f"{name} is not on the current CUDA device")
     if (c != 1 and cols > 1) or (r < cols and rows > 1):
         raise MlmcError(f"{name} must have unit inner stride and rows that do not overlap")
@@ -387,7 +388,8 @@ def _matrix(t: torch.Tensor, name: str, dtype=None, n: int = -1, d: int = -1) ->
 def _vector(t: Optional[torch.Tensor], name: str, d: int, dtype=torch.float32):
     if t is None:
         return None
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != d or (d > 1 and t.stride(0) != 1) or _elsewhere(t):
+    at = t.get_device()
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != d or not t.is_contiguous() or at < 0 or at != torch._C._cuda_getDevice():
         raise MlmcError(f"{name} must be a contiguous tensor of {dtype}, [{d}], on the current CUDA device")
     return t.data_ptr()
 
@@ -403,7 +405,7 @@ def _scratch(ws: Optional[torch.Tensor], need: int, like: torch.Tensor):
     if ws is None:
         if need == 0:
             return None, 0, None
-        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+        ws = like.new_empty(need, dtype=torch.uint8)
     elif ws.dtype is not torch.uint8 or not ws.is_contiguous() or _elsewhere(ws):
         raise MlmcError("ws must be a contiguous tensor of torch.uint8 on the current CUDA device")
     return ws.data_ptr(), ws.numel(), ws
@@ -593,7 +595,7 @@ def _eight_bits(n: int, d: int, like: torch.Tensor):
 
 
 def _same(x: torch.Tensor, n: int, d: int) -> torch.Tensor:
-    return torch.empty_like(x) if x.is_contiguous() else x.new_empty((n, d))     # the former takes less time
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(n, d)     # the former takes less time
 
 
 def _or_none(t: Optional[torch.Tensor], name: str, dtype, n: int, d: int):
@@ -648,7 +650,7 @@ def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
             ldq = _matrix(q, "q", _E4M3, n, d)
         p_q = q.data_ptr()
         if scale is None:
-            scale = torch.empty(n, dtype=torch.float32, device=x.device)
+            scale = x.new_empty(n, dtype=torch.float32)
             p_scale = scale.data_ptr()
         else:
             p_scale = _vector(scale, "scale", n)
@@ -659,7 +661,7 @@ def mlmc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
     if rstd is not None:
         p_rstd = _vector(rstd, "rstd", n)
     elif with_rstd:
-        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+        rstd = x.new_empty(n, dtype=torch.float32)
         p_rstd = rstd.data_ptr()
     rc = lib().mlmc_rms_norm(x.data_ptr(), ldx, p_r, ldr, n, d, _DTYPE[dtype], _vector(weight, "weight", d), eps, p_s, lds, p_y, ldy, p_q, ldq, p_scale, p_rstd, _stream())
     if rc:
@@ -704,7 +706,7 @@ def mlmc_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Opti
     else:
         ldq = _matrix(q, "q", _E4M3, n, d)
     if scale is None:
-        scale = torch.empty(n, dtype=torch.float32, device=x.device)
+        scale = x.new_empty(n, dtype=torch.float32)
         p_scale = scale.data_ptr()
     else:
         p_scale = _vector(scale, "scale", n)
@@ -725,7 +727,7 @@ def mlmc_linear_q8(x: torch.Tensor, x_scale: torch.Tensor, weight: torch.Tensor,
     if x_scale is None or w_scale is None:
         raise MlmcError("matrices in 8 bits need their scales")
     if y is None:
-        y, ldy = torch.empty((n, m), dtype=torch.bfloat16, device=x.device), m
+        y, ldy = x.new_empty(n, m, dtype=torch.bfloat16), m
     else:
         ldy = _matrix(y, "y", torch.bfloat16, n, m)
     p, nbytes, ws = _scratch(ws, mlmc_linear_q8_workspace(n, m, k), x)
@@ -764,18 +766,17 @@ def mlmc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = N
     dev_status (int32 [1]), if given, receives MLMC_DEV_RANGE for a token outside the vocabulary."""
     ldl = _matrix(logits, "logits")
     n, v = logits.shape
-    at = logits.device
     given, p_t, logprob = 0, None, None
     if tokens is not None:
         given = _given(tokens)
         p_t = _answers(tokens, "tokens", n, torch.int32)
-        logprob = torch.empty(tokens.shape, dtype=torch.float32, device=at)
-    entropy = torch.empty(n, dtype=torch.float32, device=at) if with_entropy else None
-    stats = torch.empty((n, 3), dtype=torch.float32, device=at) if with_stats else None
+        logprob = torch.empty_like(tokens, dtype=torch.float32)     # tokens are contiguous
+    entropy = logits.new_empty(n, dtype=torch.float32) if with_entropy else None
+    stats = logits.new_empty(n, 3, dtype=torch.float32) if with_stats else None
     top_idx = top_logprob = None
     if top > 0:
-        top_idx = torch.empty((n, top), dtype=torch.int32, device=at)
-        top_logprob = torch.empty((n, top), dtype=torch.float32, device=at)
+        top_logprob = logits.new_empty(n, top, dtype=torch.float32)
+        top_idx = torch.empty_like(top_logprob, dtype=torch.int32)
     p, nbytes, ws = _scratch(ws, mlmc_token_logprobs_workspace(n, v, top), logits)
     rc = lib().mlmc_token_logprobs(logits.data_ptr(), ldl, n, v, _DTYPE[logits.dtype], p_t, given, top, temperature,
                                    None if logprob is None else logprob.data_ptr(), None if entropy is None else entropy.data_ptr(),
