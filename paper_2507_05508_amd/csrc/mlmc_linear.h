@@ -129,7 +129,7 @@ struct Epilogue {
         constexpr int DT = RESULT<MT>;
         if (MT == DT_E4M3) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = v[e] * row_scale * col_scale[e];
+            for (int e = 0; e < 8; ++e) v[e] *= row_scale * col_scale[e];
         }
         if (g.bias) {
 #pragma unroll
@@ -662,7 +662,7 @@ template <int DT, bool WIDE> __global__ __launch_bounds__(FEW_WAVES * 64) void k
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < FEW_WAVES; ++w) v += part[w][i][threadIdx.x & 15];
-    if (DT == DT_E4M3) v = v * g.row_scale[i] * g.col_scale[j];
+    if (DT == DT_E4M3) v *= g.row_scale[i] * g.col_scale[j];
     if (g.bias) v += g.bias[j];
     if (g.z) store_as(g.z, i * g.ldz + j, RESULT<DT>, v);
     if (g.act == MLMC_ACT_GELU) v = gelu<RESULT<DT>>(v);

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
                             float v[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                v[e] = fmaf(acc[m][n][q * 4 + e] * rs[m], cs[e], bs[e]);
+                                v[e] = fmaf(acc[m][n][q * 4 + e], rs[m] * cs[e], bs[e]);
                                 if (ACT == MLMC_ACT_GELU) v[e] = gelu<MLMC_BF16>(v[e]);
                                 if (ACT == MLMC_ACT_RELU) v[e] = relu(v[e]);
                             }

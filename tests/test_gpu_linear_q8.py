@@ -101,6 +101,15 @@ def test_linear_q8_scales():
     assert x.shape == (4, 64)
 
 
+@pytest.mark.parametrize("n,m,k", [(3, 40, 512), (40, 40, 512), (128, 128, 8192), (4096, 4096, 512)])
+def test_linear_q8_scales_are_multiplied_first(n, m, k):
+    """Rows as large as fp32 has them with weights as small: the sum times either scale is not a number of fp32, the result is one of bf16."""
+    x, w = eight(torch.full((n, k), 448.0, device="cuda")), eight(torch.full((m, k), 448.0, device="cuda"))
+    for a, b in ((2.0 ** 119, 2.0 ** -60), (2.0 ** -60, 2.0 ** 119)):
+        y = P.mlmc_linear_q8(x, torch.full((n,), a, device="cuda"), w, torch.full((m,), b, device="cuda"))
+        assert bool((y == 448.0 * 448.0 * k * 2.0 ** 59).all())      # 49 of a power of two: exact
+
+
 def test_linear_q8_kernels():
     """The ways that the plan has: few rows, tiles, parts of the contraction, rows copied to aligned ones."""
     def run(n, m, k, pad=0):
