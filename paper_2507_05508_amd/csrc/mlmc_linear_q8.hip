@@ -12,10 +12,8 @@ namespace mlmc {
 // Loads and barriers as in k_linear_tile; a wave's fragments of the next half step are read over those of this one, A's as soon as its instructions have gone out.
 // 8192 x 4096 x 4096: 107 us (2.57 PFLOP/s; a library product without the epilogue 89 to 98), with gelu 121; by 8 waves of 128 x 64 (k_linear_tile) 20 more; by two workgroups a CU, 128 x 256 each and
 // steps of 64 bytes, 45 more: half as much again comes from the L2.
-constexpr int BIG = 256, BIG_T = 256, BIG_F = 4;   // (a thread for every row of the tile)
+constexpr int BIG = 256, BIG_T = 256, BIG_F = 4, AHEAD = 2;   // (a thread for every row of the tile)
 using v2b = __bf16 __attribute__((ext_vector_type(2)));
-using v4b = __bf16 __attribute__((ext_vector_type(4)));
-using v4b_u = __bf16 __attribute__((ext_vector_type(4), aligned(2)));   // at any entry's place
 
 // Chunk k of lane l of four becomes chunk l of lane k.
 __device__ inline void transpose_fours(chunk_t (&c)[4], int lane) {
@@ -165,6 +163,32 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         float rs[F];   // ahead of the next tile's loads: what is waited for comes in order
 #pragma unroll
         for (int m = 0; m < F; ++m) rs[m] = g.row_scale[min(oi + m * 32, g.I - 1)];
+        // A lane has four neighbouring entries of a row in four registers (the operands are exchanged).  Rounded and exchanged between the halves of the wave they are 64 bytes of a pair of fragments,
+        // and transposed among four lanes, 16 bytes each of the 64 of one row: a store has whole sectors of 16 rows.  (16 bytes of each of 64 places a store: 126 us instead of 115, and twice
+        // the bytes written to HBM; by way of LDS the waits of the one wave a SIMD took more than that gave.)
+        // The residual comes the same way back, the loads of four blocks of 64 columns ahead of their use.
+        const int64_t is = i0_done + wm * 128 + (lane & 28), js = oj + half * 32 + (lane & 3) * 8;
+        chunk_t ahead[AHEAD][4];
+        const auto load_residual = [&](int block) __attribute__((always_inline)) {
+            const int p = block / F, m = block % F;
+            const int left = (int)min(g.J - js - p * 64, (int64_t)8);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const __bf16* from = (const __bf16*)g.residual + min(is + m * 32 + r, g.I - 1) * g.ldr + js + p * 64;
+                if (left == 8) ahead[block % AHEAD][r] = *(const chunk_u*)from;
+                else {
+                    v8b u = {};
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < left) u[e] = from[e];
+                    ahead[block % AHEAD][r] = __builtin_bit_cast(chunk_t, u);
+                }
+            }
+        };
+        if (g.residual) {
+#pragma unroll
+            for (int b = 0; b < AHEAD; ++b) load_residual(b);
+        }
         k += gridDim.x;
         const bool again = k < tiles;
         if (again) {
@@ -172,24 +196,36 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
             A.fetch(a0, 0, c_whole);
             B.fetch(b0, 0, c_whole);
         }
-        // A lane has four neighbouring entries of a row in four registers (the operands are exchanged).  Rounded and exchanged between the halves of the wave they are 64 bytes of a pair of fragments,
-        // and transposed among four lanes, 16 bytes each of the 64 of one row: a store has whole sectors of 16 rows.  (16 bytes of each of 64 places a store: 126 us instead of 115, and twice
-        // the bytes written to HBM; by way of LDS the waits of the one wave a SIMD took more than that gave.)
-        const auto results = [&](auto act, auto whole) __attribute__((always_inline)) {
+        const auto results = [&](auto act, auto residual) __attribute__((always_inline)) {
             constexpr int ACT = decltype(act)::value;
-            constexpr bool WHOLE = decltype(whole)::value;   // all columns of the tile
-            const int64_t is = i0_done + wm * 128 + (lane & 28), js = oj + half * 32 + (lane & 3) * 8;
+            constexpr bool RES = decltype(residual)::value;
             __bf16* const y = (__bf16*)g.out + is * g.ldo + js;
 #pragma unroll
             for (int p = 0; p < F / 2; ++p)
 #pragma unroll
                 for (int m = 0; m < F; ++m) {
                     __builtin_amdgcn_sched_barrier(0);   // one after the other: there are no registers for more
-                    chunk_t out[4];
+                    chunk_t out[4], add[4];
+                    if (RES) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) add[r] = ahead[(p * F + m) % AHEAD][r];
+                        transpose_fours(add, lane);
+                        if (p * F + m + AHEAD < F * F / 2) load_residual(p * F + m + AHEAD);
+                    }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int n = 2 * p + k;
-                        unsigned packed[4][2];
+                        unsigned packed[4][2], added[4][2];
+                        if (RES) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int w = 0; w < 2; ++w) {
+                                    const auto both = __builtin_amdgcn_permlane32_swap(add[2 * k + h][w], add[2 * k + h][2 + w], false, false);
+                                    added[h][w] = both[0];
+                                    added[2 + h][w] = both[1];
+                                }
+                        }
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             const int col = p * 64 + (q >> 1) * 32 + k * 16 + (q & 1) * 8 + half * 4;
@@ -200,18 +236,7 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
                                 v[e] = fmaf(acc[m][n][q * 4 + e], rs[m] * cs[e], bs[e]);
                                 if (ACT == MLMC_ACT_GELU) v[e] = gelu<MLMC_BF16>(v[e]);
                                 if (ACT == MLMC_ACT_RELU) v[e] = relu(v[e]);
-                            }
-                            if (g.residual) {
-                                const __bf16* r = (const __bf16*)g.residual + min(oi + m * 32, g.I - 1) * g.ldr + oj + col;
-                                if (WHOLE) {
-                                    const v4b u = *(const v4b_u*)r;
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) v[e] += (float)u[e];
-                                } else {
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e)
-                                        if (oj + col + e < g.J) v[e] += (float)r[e];
-                                }
+                                if (RES) v[e] += (float)__builtin_bit_cast(v2b, added[q][e / 2])[e & 1];
                             }
 #pragma unroll
                             for (int w = 0; w < 2; ++w) packed[q][w] = __builtin_bit_cast(unsigned, v2b{(__bf16)v[2 * w], (__bf16)v[2 * w + 1]});
@@ -226,22 +251,23 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
                             }
                     }
                     transpose_fours(out, lane);
+                    const int left = (int)min(g.J - js - p * 64, (int64_t)8);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         if (is + m * 32 + r >= g.I) continue;
                         __bf16* to = y + (m * 32 + r) * g.ldo + p * 64;
-                        if (WHOLE) *(chunk_u*)to = out[r];
+                        if (left == 8) *(chunk_u*)to = out[r];
                         else {
                             const v8b u = __builtin_bit_cast(v8b, out[r]);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (js + p * 64 + e < g.J) to[e] = u[e];
+                            for (int e = 0; e < 7; ++e)
+                                if (e < left) to[e] = u[e];
                         }
                     }
                 }
         };
         const auto results_of = [&](auto act) __attribute__((always_inline)) {
-            if (oj - wn * 128 + BIG <= g.J) results(act, std::true_type{});
+            if (g.residual) results(act, std::true_type{});
             else results(act, std::false_type{});
         };
         if (g.act == MLMC_ACT_GELU) results_of(std::integral_constant<int, MLMC_ACT_GELU>{});
