@@ -689,6 +689,9 @@ constexpr TileCost tile_costs[TILES] = {{32, 128, {0.55f, 0.42f}, {0.53f, 0.28f}
                                         {128, 128, {1.85f, 0.70f}, {1.85f, 0.50f}, 2.5f}, {256, 256, {0.f, 1.50f}, {0.f, 1.60f}, 11.f}};
 // The large tile of 8 bits: 8192 x 4096 x 4096 107 us, 4096 x 4096 x 4096 56, by tiles of 128 159 and 69.
 constexpr TileCost q8_big_cost = {256, 256, {0.f, 1.35f}, {0.f, 1.35f}, 9.f};
+// What gelu (1), a residual (2) or both add to a round of 8 bits: nothing else runs on a CU meanwhile where its tile is large.  Large tiles / tiles of 128, both, us: 13320 x 2048 x 512 70 / 58,
+// 4000 x 4000 x 128 42 / 29, 16384 x 1024 x 1024 43 / 40, 8192 x 4096 x 1024 86 / 88, 8192 x 4096 x 2048 111 / 124; neither: 34 / 41, 19 / 18, 25 / 31, 48 / 56, 69 / 83.
+constexpr float q8_epilogue_us[4] = {0.f, 1.3f, 1.5f, 2.5f}, q8_big_epilogue_us[4] = {0.f, 9.f, 6.5f, 18.f};   // of 128 x 128 entries, of the large tile
 constexpr float LAUNCH_US = 5.f, JOIN_US = 3.f, JOIN_ENTRY_US = 1.6e-6f;
 constexpr int LINEAR_CUS = 256, SPLITS_MAX = 32;
 
@@ -697,7 +700,7 @@ static int entry_bytes(int dtype) { return dtype == MLMC_F32 ? 4 : dtype == MLMC
 
 // The tile and the number of parts of the contraction that the costs above say to be the fastest: tiles come in rounds of one for every CU, a part more
 // makes the rounds finer and the join longer.
-static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool fast) {
+static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool fast, int epilogue = 0) {
     const int step = 128 / entry_bytes(dtype), cost = dtype == MLMC_F32 ? 0 : 1;   // a step of 8 bits has the loads of one of 16, and matrix instructions of twice the entries in the same time
     const int64_t steps = (C + step - 1) / step;
     LinearPlan best = {TILE_128, 1, (int)C, 0.f};
@@ -706,10 +709,11 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
         if (t == TILE_256 && (dtype == MLMC_F32 || !fast)) continue;
         const TileCost& k = dtype == DT_E4M3 && t == TILE_256 ? q8_big_cost : tile_costs[t];
         const int64_t tiles = ((I + k.rows - 1) / k.rows) * ((J + k.cols - 1) / k.cols);
+        const float end_us = t == TILE_256 ? q8_big_epilogue_us[epilogue] : q8_epilogue_us[epilogue] * (float)(k.rows * k.cols) / 16384.f;
         for (int s = 1; s <= (dtype == DT_E4M3 && t == TILE_256 ? 1 : SPLITS_MAX) && (s == 1 || (s * 2 <= steps && tiles * (s - 1) < 2 * LINEAR_CUS)); ++s) {
             const int64_t len = (steps + s - 1) / s, parts = steps ? (steps + len - 1) / len : 1, rounds = (tiles * parts + LINEAR_CUS - 1) / LINEAR_CUS;
             if (parts != s) continue;
-            const float us = LAUNCH_US + (float)rounds * (k.round_us + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
+            const float us = LAUNCH_US + (float)rounds * (k.round_us + (s == 1 ? end_us : 0.f) + (float)len * (rounds == 1 ? k.alone_us : k.among_us)[cost]) +
                              (s > 1 ? JOIN_US + JOIN_ENTRY_US * (float)(s * I) * (float)J : 0.f);
             if (us < least) {
                 least = us;
@@ -759,13 +763,13 @@ static int operand_way(const void* p, int64_t ld, int64_t width, bool along, int
 // 1001 x 1999 x 1535 23 / 20, 48 / 32, 32 / 26; 12175 x 1037 x 613 50 / 48, 50 / 44, 73 / 52.
 struct PackPlan { bool pack; LinearPlan plan; size_t bytes[2]; };
 static size_t packed_bytes(int64_t rows, int64_t cols, int E) { return (size_t)rows * (size_t)((cols + E - 1) / E) * 16; }
-static PackPlan pack_plan(int64_t I, int64_t J, int64_t C, int dtype, bool aa, bool ba, int way, bool pack_a, bool pack_b) {
+static PackPlan pack_plan(int64_t I, int64_t J, int64_t C, int dtype, bool aa, bool ba, int way, bool pack_a, bool pack_b, int epilogue = 0) {
     const int E = 16 / entry_bytes(dtype);
-    PackPlan r = {false, linear_plan(I, J, C, dtype, false), {0, 0}};
+    PackPlan r = {false, linear_plan(I, J, C, dtype, false, epilogue), {0, 0}};
     const int64_t a_cols = aa ? C : I, a_rows = aa ? I : C, b_cols = ba ? C : J, b_rows = ba ? J : C;
     const bool even = a_cols % E == 0 && b_cols % E == 0 && dtype == MLMC_BF16;   // bf16 by widths alone
     if (even || a_cols < E || b_cols < E || a_rows * ((a_cols + E - 1) / E) >= ((int64_t)1 << 30) || b_rows * ((b_cols + E - 1) / E) >= ((int64_t)1 << 30)) return r;
-    const LinearPlan fast = linear_plan(I, J, C, dtype, true);
+    const LinearPlan fast = linear_plan(I, J, C, dtype, true, epilogue);
     const size_t a = pack_a ? packed_bytes(a_rows, a_cols, E) : 0, b = pack_b ? packed_bytes(b_rows, b_cols, E) : 0;
     const float slower = way == WAY_WORDS || (aa && ba) ? 1.5f : 2.1f, copy_us = LAUNCH_US + 2.0f * (float)(a + b) / 3.0e6f;
     if (fast.us + copy_us >= slower * r.plan.us) return r;
@@ -801,17 +805,18 @@ template <int DT, bool AA, bool BA> static mlmc_status linear_layout(LinearArgs 
     const int wa = operand_way(g.a, g.lda, AA ? g.C : g.I, AA, esize), wb = operand_way(g.b, g.ldb, BA ? g.C : g.J, BA, esize);
     int way = wa == WAY_REGISTERS || wb == WAY_REGISTERS ? WAY_REGISTERS : wa == WAY_CHUNKS && wb == WAY_CHUNKS ? WAY_CHUNKS : WAY_WORDS;
     if (DT == DT_E4M3 && way == WAY_WORDS) way = WAY_REGISTERS;
+    const int epilogue = DT != DT_E4M3 ? 0 : (g.act == MLMC_ACT_GELU ? 1 : 0) + (g.residual ? 2 : 0);
     LinearPlan p;
     size_t packed[2] = {0, 0};
     if (DT != MLMC_F32 && way != WAY_CHUNKS && g.C > 0) {
-        const PackPlan k = pack_plan(g.I, g.J, g.C, DT, AA, BA, way, wa != WAY_CHUNKS, wb != WAY_CHUNKS);
+        const PackPlan k = pack_plan(g.I, g.J, g.C, DT, AA, BA, way, wa != WAY_CHUNKS, wb != WAY_CHUNKS, epilogue);
         p = k.plan;
         if (k.pack) {
             way = WAY_CHUNKS;
             packed[0] = k.bytes[0];
             packed[1] = k.bytes[1];
         }
-    } else p = linear_plan(g.I, g.J, g.C, DT, way == WAY_CHUNKS);
+    } else p = linear_plan(g.I, g.J, g.C, DT, way == WAY_CHUNKS, epilogue);
     g.splits = p.splits;
     g.split_len = p.split_len;
     const size_t parts = align256(linear_part_bytes(p, g.I, g.J)), need = parts + align256(packed[0]) + packed[1];

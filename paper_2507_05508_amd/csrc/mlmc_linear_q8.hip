@@ -166,7 +166,8 @@ __global__ __launch_bounds__(BIG_T, 1) void k_linear_q8(LinearArgs g) {
         // A lane has four neighbouring entries of a row in four registers (the operands are exchanged).  Rounded and exchanged between the halves of the wave they are 64 bytes of a pair of fragments,
         // and transposed among four lanes, 16 bytes each of the 64 of one row: a store has whole sectors of 16 rows.  (16 bytes of each of 64 places a store: 126 us instead of 115, and twice
         // the bytes written to HBM; by way of LDS the waits of the one wave a SIMD took more than that gave.)
-        // The residual comes the same way back, the loads of four blocks of 64 columns ahead of their use.
+        // The residual comes the same way back, loaded two blocks of 32 rows and 64 columns ahead of its use (more spill registers; by way of the free pair of buffers all of it took half as long again).
+        // 8192 x 4096 x 4096 with residual 136 us (by 8 bytes a lane of 32 rows, without loads ahead, 150), 4000 x 4001 x 1072 50 (86).
         const int64_t is = i0_done + wm * 128 + (lane & 28), js = oj + half * 32 + (lane & 3) * 8;
         chunk_t ahead[AHEAD][4];
         const auto load_residual = [&](int block) __attribute__((always_inline)) {
@@ -297,14 +298,16 @@ extern "C" {
 size_t mlmc_linear_q8_workspace(int64_t rows, int64_t outputs, int64_t inputs) {
     if (!linear_sizes_ok(rows, outputs, inputs) || rows == 0 || few_rows(rows, outputs, inputs, DT_E4M3)) return 0;
     size_t most = 0;
-    for (bool fast : {false, true}) {
-        const size_t need = align256(linear_part_bytes(linear_plan(rows, outputs, inputs, DT_E4M3, fast), rows, outputs));
-        most = need > most ? need : most;
-    }
-    for (int which = 1; which < 4; ++which) {
-        const PackPlan k = pack_plan(rows, outputs, inputs, DT_E4M3, true, true, WAY_REGISTERS, which & 1, which & 2);
-        const size_t need = align256(linear_part_bytes(k.plan, rows, outputs)) + align256(k.bytes[0]) + k.bytes[1];
-        most = need > most ? need : most;
+    for (int epilogue = 0; epilogue < 4; ++epilogue) {
+        for (bool fast : {false, true}) {
+            const size_t need = align256(linear_part_bytes(linear_plan(rows, outputs, inputs, DT_E4M3, fast, epilogue), rows, outputs));
+            most = need > most ? need : most;
+        }
+        for (int which = 1; which < 4; ++which) {
+            const PackPlan k = pack_plan(rows, outputs, inputs, DT_E4M3, true, true, WAY_REGISTERS, which & 1, which & 2, epilogue);
+            const size_t need = align256(linear_part_bytes(k.plan, rows, outputs)) + align256(k.bytes[0]) + k.bytes[1];
+            most = need > most ? need : most;
+        }
     }
     return most;
 }

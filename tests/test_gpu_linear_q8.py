@@ -110,6 +110,25 @@ def test_linear_q8_scales_are_multiplied_first(n, m, k):
         assert bool((y == 448.0 * 448.0 * k * 2.0 ** 59).all())      # 49 of a power of two: exact
 
 
+@pytest.mark.parametrize("n,m,k,pad", [(4096, 4096, 4096, 0), (4090, 4003, 4096, 1), (50, 300, 1000, 3), (1000, 1000, 256, 0)])
+def test_linear_q8_gelu_and_residual(n, m, k, pad):
+    """The sum with a residual is that of what the call gives without one, but for the rounding of either to 16 bits; in the residual's place, too."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n + m)
+    x, xs = P.mlmc_quantize(torch.empty((n, k), device="cuda").normal_(generator=gen))
+    w, ws = P.mlmc_quantize(torch.empty((m, k), device="cuda").normal_(0.0, k ** -0.5, generator=gen))
+    r = torch.empty((n, m + pad), device="cuda").normal_(0.0, 4.0, generator=gen).to(torch.bfloat16)[:, :m]
+    bare = P.mlmc_linear_q8(x, xs, w, ws, act=ACT["gelu"]).double()
+    if k == 4096:
+        assert launched(lambda: P.mlmc_linear_q8(x, xs, w, ws, act=ACT["gelu"], residual=r)) == {"k_linear_q8"}
+    y = P.mlmc_linear_q8(x, xs, w, ws, act=ACT["gelu"], residual=r)
+    want = bare + r.double()
+    # both plans may differ in the order of their sums: 2^-14 of a result of size 1 covers that
+    assert bool(((y.double() - want).abs() <= 1.01 * 2.0 ** -8 * (bare.abs() + want.abs()) + 2.0 ** -14).all())
+    P.mlmc_linear_q8(x, xs, w, ws, act=ACT["gelu"], residual=r, y=r)
+    assert torch.equal(r, y)
+
+
 def test_linear_q8_kernels():
     """The ways that the plan has: few rows, tiles, parts of the contraction, rows copied to aligned ones."""
     def run(n, m, k, pad=0):
