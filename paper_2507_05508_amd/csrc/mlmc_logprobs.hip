@@ -149,7 +149,7 @@ template <int DT> __global__ __launch_bounds__(STRETCH_WG, 8) void k_logprobs(Lo
 // ---- rows ---------------------------------------------------------------------------------------------------------------------------------
 
 constexpr int ROOM = 1024, LIST = 512, BATCH = 4;   // keys found, groups listed; loads in flight
-constexpr int SHORT_CHUNKS = 1024;                  // of a row that one workgroup has in its registers
+constexpr int SHORT_N = 4, SHORT_CHUNKS = 1024 * SHORT_N;   // chunks of a thread, and of a row, that one workgroup has in its registers
 
 // Lanes below this one that are in the mask.
 __device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
@@ -325,15 +325,15 @@ template <int N, int E> __device__ inline void collect(const float (&f)[N][E], f
             }
 }
 // The n keys found, each at its place.
-__device__ inline void write_found(const LogprobArgs& a, int64_t row, const uint64_t* found, int n, const RowSums& sums) {
-    for (int i = threadIdx.x; i < n; i += ROWS_T) {
+template <int T> __device__ inline void write_found(const LogprobArgs& a, int64_t row, const uint64_t* found, int n, const RowSums& sums) {
+    for (int i = threadIdx.x; i < n; i += T) {
         const uint64_t key = found[i];
         int before = 0;
 #pragma unroll 8
         for (int o = 0; o < n; ++o) before += found[o] > key;
         if (before < a.top) write_top(a, row, before, key, sums);
     }
-    for (int i = n + threadIdx.x; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+    for (int i = n + threadIdx.x; i < a.top; i += T) write_top(a, row, i, 0, sums);
 }
 __device__ inline void write_sums(const LogprobArgs& a, int64_t row, int32_t token, float logit, const RowSums& sums) {
     const int t = threadIdx.x;
@@ -463,16 +463,16 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
             __syncthreads();
             n = number;
         }
-        write_found(a, row, found, n, sums);
+        write_found<ROWS_T>(a, row, found, n, sums);
     }
 }
 
-// A short row (up to 1024 chunks of 16 bytes) by a workgroup, all of it in its registers: a chunk is a group, and its entries are at hand.
-template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logprobs_short(LogprobArgs a) {
-    constexpr int E = ENTRIES<DT>, N = SHORT_CHUNKS / ROWS_T, W = ROWS_T / 64;
+// A short row (up to 4 T chunks of 16 bytes) by a workgroup of T threads, all of it in its registers: a chunk is a group, and its entries are at hand.
+template <int DT, int T, bool TOP> __global__ __launch_bounds__(T, 8) void k_logprobs_short(LogprobArgs a) {
+    constexpr int E = ENTRIES<DT>, N = SHORT_N, W = T / 64;
     __shared__ uint64_t found[TOP ? ROOM : 1];
     __shared__ uint32_t list[TOP ? 2 * MOST_ANSWERS : 1];
-    __shared__ float groups[TOP ? SHORT_CHUNKS : 1];
+    __shared__ float groups[TOP ? N * T : 1];
     __shared__ __align__(16) int bins[TOP ? BINS : 1];
     __shared__ float most[W], lows[W], part[2][W];
     __shared__ int number;
@@ -482,14 +482,14 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
     chunk_t v[N];
 #pragma unroll
     for (int n = 0; n < N; ++n)
-        if (n * ROWS_T * E < vocab) v[n] = load_chunk<DT>(s, (n * ROWS_T + t) * E, vocab);
+        if (n * T * E < vocab) v[n] = load_chunk<DT>(s, (n * T + t) * E, vocab);
     float logit;
     const int32_t token = load_token<DT>(a, row, logit);
     float f[E], g[N], m = -INFINITY, low = INFINITY;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         g[n] = -INFINITY;
-        if (n * ROWS_T * E >= vocab) continue;
+        if (n * T * E >= vocab) continue;
         chunk_floats<DT>(f, v[n]);
 #pragma unroll
         for (int e = 0; e < E; ++e) g[n] = fmaxf(g[n], f[e]);
@@ -503,7 +503,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
         lows[wave] = low;
     }
     if (TOP) {
-        bins[t] = 0;
+        if (t < BINS) bins[t] = 0;
         if (t == 0) number = 0;
     }
     __syncthreads();
@@ -521,7 +521,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
     float sum = 0.f, elog = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        if (n * ROWS_T * E >= vocab) continue;
+        if (n * T * E >= vocab) continue;
         chunk_floats<DT>(f, v[n]);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -547,7 +547,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
     write_sums(a, row, token, logit, sums);
     if constexpr (TOP) {
         if (sums.bad) {
-            for (int i = t; i < a.top; i += ROWS_T) write_top(a, row, i, 0, sums);
+            for (int i = t; i < a.top; i += T) write_top(a, row, i, 0, sums);
             return;
         }
         bound.find(bins, a.top);
@@ -560,8 +560,8 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
             unsigned col[N];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                col[n] = (unsigned)((n * ROWS_T + t) * E);
-                if (n * ROWS_T * E < vocab) chunk_floats<DT>(all[n], v[n]);
+                col[n] = (unsigned)((n * T + t) * E);
+                if (n * T * E < vocab) chunk_floats<DT>(all[n], v[n]);
                 else {
 #pragma unroll
                     for (int e = 0; e < E; ++e) all[n][e] = -INFINITY;
@@ -573,7 +573,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
         int n = number;
         if (n > ROOM) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) groups[k * ROWS_T + t] = g[k];
+            for (int k = 0; k < N; ++k) groups[k * T + t] = g[k];
             __syncthreads();
             if (wave == 0) {
                 n = top_by_bisection<DT>(a, s, groups, found, list);
@@ -582,7 +582,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(ROWS_T, 8) void k_logpr
             __syncthreads();
             n = number;
         }
-        write_found(a, row, found, n, sums);
+        write_found<T>(a, row, found, n, sums);
     }
 }
 
@@ -696,10 +696,13 @@ constexpr int64_t VOCAB_MAX = (int64_t)1 << 20;
 constexpr int GROUPS_MOST = 1024;   // more only of rows that have them with all lanes of a wave
 
 struct LogprobPlan { int stretches, groups, lanes; };
-static LogprobPlan logprob_plan(int64_t vocab, int dtype, int top) {
+// Rows of up to 2048 chunks by one workgroup each; up to 4096 where all workgroups of 1024 threads are on the chip at once, or without alternatives, whose search holds up the next row's loads.
+// In one launch / in two, us: 4 x 32000 bf16 with 20 13.1 / 15.6 (bound by the host), 512 x 32768 with 128 19.5 / 21.6, 2048 x 32000 with 20 51.8 / 40.1, without 4000 x 32000 49.9 / 51.4;
+// of 512 threads 8000 x 8000 fp32 with 20 63 / 80, 8000 x 12000 bf16 with 64 80 / 91.
+static LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int dtype, int top) {
     const int64_t E = dtype == MLMC_BF16 ? 8 : 4, stretch = 64 * STRETCH_N * E, chunks = (vocab + E - 1) / E;
     LogprobPlan p = {(int)((vocab + stretch - 1) / stretch), 0, 1};
-    if (chunks <= SHORT_CHUNKS) return {0, (int)chunks, 1};   // by one workgroup, without a workspace
+    if (chunks <= (rows <= 512 || !top ? SHORT_CHUNKS : SHORT_CHUNKS / 2)) return {0, (int)chunks, 1};   // by one workgroup, without a workspace
     while (p.lanes < 64 && (chunks + p.lanes - 1) / p.lanes > GROUPS_MOST) p.lanes *= 2;
     if (top) p.groups = (int)((chunks + p.lanes - 1) / p.lanes);
     return p;
@@ -711,13 +714,18 @@ static bool logprob_sizes_ok(int64_t rows, int64_t vocab, int given, int top) {
 static bool temperature_ok(float t) { return t > 0.0f && t <= 3.402823e38f && 1.4426950408889634f / t <= 3.402823e38f; }
 constexpr int64_t ROW_SLICE = 32768;   // rows of a launch: they are the grid's second axis
 
+template <int DT, int T> static mlmc_status logprob_short(const LogprobArgs& a, unsigned rows, hipStream_t st) {
+    if (a.top) MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, T, true><<<rows, T, 0, st>>>(a)));
+    else MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, T, false><<<rows, T, 0, st>>>(a)));
+    return MLMC_OK;
+}
 template <int DT> static mlmc_status logprob_run(LogprobArgs a, hipStream_t st) {
     const int each = a.stretches < STRETCH_WG / 64 ? a.stretches : STRETCH_WG / 64;
     for (; a.row0 < a.rows; a.row0 += ROW_SLICE) {
         const unsigned rows = (unsigned)(a.rows - a.row0 < ROW_SLICE ? a.rows - a.row0 : ROW_SLICE);
         if (a.stretches == 0) {
-            if (a.top) MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, true><<<rows, ROWS_T, 0, st>>>(a)));
-            else MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs_short<DT, false><<<rows, ROWS_T, 0, st>>>(a)));
+            const mlmc_status rc = a.groups <= 256 * SHORT_N ? logprob_short<DT, 256>(a, rows, st) : a.groups <= 512 * SHORT_N ? logprob_short<DT, 512>(a, rows, st) : logprob_short<DT, 1024>(a, rows, st);
+            if (rc != MLMC_OK) return rc;
             continue;
         }
         MLMC_LAUNCH(K_LOGPROBS, st, (k_logprobs<DT><<<dim3((unsigned)((a.stretches + each - 1) / each), rows), each * 64, 0, st>>>(a)));
@@ -745,7 +753,7 @@ extern "C" {
 
 size_t mlmc_token_logprobs_workspace(int64_t rows, int64_t vocab, int top) {
     if (!logprob_sizes_ok(rows, vocab, 0, top) || rows == 0) return 0;
-    const size_t a = logprob_bytes(logprob_plan(vocab, MLMC_F32, top), rows), b = logprob_bytes(logprob_plan(vocab, MLMC_BF16, top), rows);
+    const size_t a = logprob_bytes(logprob_plan(rows, vocab, MLMC_F32, top), rows), b = logprob_bytes(logprob_plan(rows, vocab, MLMC_BF16, top), rows);
     return a > b ? a : b;
 }
 
@@ -760,7 +768,7 @@ mlmc_status mlmc_token_logprobs(const void* logits, int64_t ldl, int64_t rows, i
         if (given && (!tokens || !f32_ptr_ok(tokens) || !logprob || !f32_ptr_ok(logprob))) return MLMC_EINVAL;
         if (top && (!top_idx || !f32_ptr_ok(top_idx) || !top_logprob || !f32_ptr_ok(top_logprob))) return MLMC_EINVAL;
     }
-    const LogprobPlan p = logprob_plan(vocab, dtype, top);
+    const LogprobPlan p = logprob_plan(rows, vocab, dtype, top);
     const size_t need = logprob_bytes(p, rows);
     if (rows > 0 && need && (!ws || (uintptr_t)ws % 256 || ws_bytes < need)) return MLMC_EINVAL;
     if (dev_status) MLMC_LAUNCH(K_ZERO, st, (k_logprobs_clear<<<1, 1, 0, st>>>(dev_status)));

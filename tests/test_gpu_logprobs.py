@@ -19,7 +19,7 @@ INF, NAN = math.inf, math.nan
 SIZES = [  # rows, vocabulary, pad, shift, given, top
     (1, 1, 0, 0, 1, 1), (3, 2, 1, 1, 2, 5), (2, 7, 0, 0, 1, 3), (5, 64, 0, 0, 1, 0), (4, 129, 3, 1, 0, 7), (33, 1000, 0, 0, 1, 20), (9, 1023, 1, 3, 7, 128), (600, 257, 0, 0, 1, 5),
     (600, 5000, 0, 0, 1, 64), (3, 8191, 2, 0, 4, 64), (520, 8200, 0, 0, 1, 20), (2, 32768, 0, 0, 1, 128), (2, 50021, 3, 2, 1, 20), (1, 131072, 0, 0, 128, 128), (515, 33000, 0, 0, 1, 10),
-    (2, 262147, 0, 1, 1, 64), (513, 66000, 0, 0, 1, 64),
+    (2, 262147, 0, 1, 1, 64), (513, 66000, 0, 0, 1, 64), (40, 16000, 0, 0, 1, 64), (7, 16383, 1, 1, 3, 128), (520, 16390, 0, 0, 1, 20),
 ]
 
 
@@ -72,7 +72,7 @@ def test_token_logprobs(n, v, pad, shift, given, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,v", [(600, 700), (600, 9000), (3, 9000), (2, 70001), (515, 33000), (513, 66000)])
+@pytest.mark.parametrize("n,v", [(600, 700), (600, 9000), (3, 9000), (40, 16000), (520, 15000), (9, 31000), (2, 70001), (515, 33000), (513, 66000)])
 def test_ties_orders_and_masks(n, v, dtype):
     """Equal logits, rows in ascending and descending order, rows of which few entries are left, a lowest value as a mask: the alternatives are those of a stable sort."""
     rng = np.random.default_rng(v)
@@ -219,11 +219,14 @@ def test_large_temperatures_and_logits():
 
 
 def test_kernels():
-    """A workgroup has a short row, longer ones take two launches."""
-    x, y = torch.zeros((600, 4096), device="cuda"), torch.zeros((2, 4097), device="cuda")
-    assert P.mlmc_token_logprobs_workspace(600, 4096, 3) == 0 and launched(lambda: P.mlmc_token_logprobs(x, top=3)) == {"k_logprobs"}
-    assert launched(lambda: P.mlmc_token_logprobs(y, top=3)) == launched(lambda: P.mlmc_token_logprobs(y)) == {"k_logprobs", "k_logprobs_rows"}
-    assert launched(lambda: P.mlmc_token_logprobs_backward(x, torch.zeros((600, 3), device="cuda"))) == {"k_logprobs_backward"}
+    """A workgroup has a short row, longer ones take two launches, and so do many rows of middle length with alternatives."""
+    zeros = lambda n, v: torch.zeros((n, v), device="cuda")  # noqa: E731
+    one, two = {"k_logprobs"}, {"k_logprobs", "k_logprobs_rows"}
+    for n, v, top, want in ((600, 4096, 3, one), (600, 8192, 3, one), (600, 8193, 3, two), (600, 8193, 0, one), (512, 16384, 3, one), (512, 16385, 3, two), (2, 16385, 0, two)):
+        x = zeros(n, v)
+        assert launched(lambda: P.mlmc_token_logprobs(x, top=top)) == want
+        assert (P.mlmc_token_logprobs_workspace(n, v, top) == 0) == (want is one)
+    assert launched(lambda: P.mlmc_token_logprobs_backward(x, torch.zeros((2, 3), device="cuda"))) == {"k_logprobs_backward"}
 
 
 def test_as_a_teacher_of_the_distillation_loss():

@@ -136,11 +136,11 @@ def test_on_another_stream():
 
 def test_workspaces_of_the_caller():
     """Of exactly the size asked for, filled with NaN before; 16 bytes are refused."""
-    x = batch(50, 9000, 3)
+    x, logits = batch(50, 9000, 3), batch(50, 40000, 3)
     tokens = torch.zeros((50, 1), dtype=torch.int32, device="cuda")
     q, s = P.mlmc_quantize(batch(128, 8192, 4))
     dy, rstd, dw = batch(50, 9000, 5), torch.ones(50, device="cuda"), torch.zeros(9000, device="cuda")
-    calls = ((lambda ws: P.mlmc_token_logprobs(x, tokens, top=7, with_entropy=True, ws=ws)[:4], P.mlmc_token_logprobs_workspace(50, 9000, 7)),
+    calls = ((lambda ws: P.mlmc_token_logprobs(logits, tokens, top=7, with_entropy=True, ws=ws)[:4], P.mlmc_token_logprobs_workspace(50, 40000, 7)),
              (lambda ws: (P.mlmc_linear_q8(q, s, q, s, ws=ws),), P.mlmc_linear_q8_workspace(128, 128, 8192)),
              (lambda ws: (P.mlmc_rms_norm_backward(dy, x, None, rstd, dw, ws=ws), dw.clone()), P.mlmc_rms_norm_workspace(50, 9000)))
     for call, need in calls:
