@@ -10,7 +10,7 @@ namespace mlmc {
 
 // The large tile of matrices whose rows are aligned: 256 x 256 by 4 waves of 128 x 128, a workgroup for every CU with tile after tile, the first loads of the next one ahead of the stores of the last.
 // Loads and barriers as in k_linear_tile; a wave's fragments of the next half step are read over those of this one, A's as soon as its instructions have gone out.
-// 8192 x 4096 x 4096: 107 us (2.57 PFLOP/s; a library product without the epilogue 89 to 98), with gelu 121; by 8 waves of 128 x 64 (k_linear_tile) 20 more; by two workgroups a CU, 128 x 256 each and
+// 8192 x 4096 x 4096: 107 to 119 us by the card's clock (2.57 to 2.31 PFLOP/s; a library product without the epilogue 89 to 98), with gelu 121 to 136; by 8 waves of 128 x 64 (k_linear_tile) 20 more; by two workgroups a CU, 128 x 256 each and
 // steps of 64 bytes, 45 more: half as much again comes from the L2.
 constexpr int BIG = 256, BIG_T = 256, BIG_F = 4, AHEAD = 2;   // (a thread for every row of the tile)
 using v2b = __bf16 __attribute__((ext_vector_type(2)));

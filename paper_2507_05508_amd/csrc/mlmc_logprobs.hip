@@ -11,6 +11,7 @@
 // that no entry below it is among the top K, and none of the groups that do not reach it holds one.  Those K groups are read again, of 1024 groups at most; a few more than K of their entries
 // reach the bound (of 131072 independent entries 66 for K = 64), and each counts how many are before it.  Of equal entries the first K are enough; where an order of the row brings more than the
 // room for them (a row in ascending order), those found so far are cut to the top K by bisection.
+// Shorter rows are held by one workgroup each (k_logprobs_short): its chunks are the groups, and one launch does all.
 #include "mlmc_worker.h"
 
 namespace mlmc {
