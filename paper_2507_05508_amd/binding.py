@@ -151,8 +151,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    # the handle of torch.cuda.current_stream(), without the object around it (2.7 us of a call, 0.3 this way)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    # the handle of torch.cuda.current_stream(), without the object around it (2.7 us of a call, 0.2 this way)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def mlmc_geometric_p(L: int):
