@@ -379,7 +379,7 @@ mlmc_status mlmc_distill(const void *logits, int64_t ldl, int64_t rows, int64_t 
  *   sum: dev [rows][lds] (out) or NULL: receives s; only with a residual;  y: dev [rows][ldy] (out) or NULL;
  *   q, scale: dev [rows][ldq] bytes and [rows] fp32 (out), or both NULL: y in 8 bits as mlmc_quantize has it;  at least one of y and q;
  *   rstd: dev [rows] fp32 (out) or NULL: r, for the backward pass.  sum and y may each be x or the residual, but not both the same matrix.
- * The sum of the squares is fp32: of rows for which it is infinite r is 0, and y the product with that.
+ * The sum of the squares is fp32: of rows for which it is infinite r is 0, of those for which it and eps are 0 r is infinite, and y the product with that; with an infinite weight, too.
  */
 mlmc_status mlmc_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int64_t rows, int64_t d, int dtype, const float *weight, float eps,
                           void *sum, int64_t lds, void *y, int64_t ldy, uint8_t *q, int64_t ldq, float *scale, float *rstd, void *hip_stream);

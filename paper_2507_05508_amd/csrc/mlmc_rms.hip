@@ -46,9 +46,10 @@ struct ToEight {
     }
     __device__ float operator()(float y, float rest) const { return fmaf(y, hi, fmaf(y, lo, rest * hi)); }   // of y + rest
 };
-// s r w, rounded once, and what that leaves over
+// s r w, rounded once, and what that leaves over.  c is a number: where w or r is infinite it is an infinity of either sign or NaN, and y is h w (the median takes the least for a NaN).
+// The median takes 8192 x 8192 bf16 from 44.4 us to 45.7 and no time with a residual; a branch for rows without infinities took 46.9, and 45.5 for 42.2 with residual and 8 bits (8192 x 4096).
 __device__ inline float normed(float s, float r, float w, float& rest) {
-    const float h = s * r, c = fmaf(s, r, -h) * w, y = fmaf(h, w, c);
+    const float h = s * r, c = __builtin_amdgcn_fmed3f(fmaf(s, r, -h) * w, -3.402823466e38f, 3.402823466e38f), y = fmaf(h, w, c);
     rest = fmaf(h, w, -y) + c;
     return y;
 }
