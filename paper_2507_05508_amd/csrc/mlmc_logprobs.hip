@@ -47,6 +47,15 @@ __device__ inline uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
 __device__ inline float key_value(uint64_t key) { return unordered((uint32_t)(key >> 32)); }
 constexpr float LOWEST = -3.402823466e38f;
 
+// (s - m) / T in the base of `unit`, m being at least s.  Differences below the range of fp32 are taken of halves, where the temperature may bring them back into it; where it is too small for
+// that they are -Inf, as they have to be.  As many instructions as the difference.
+struct Scaled {
+    float half, m, unit;
+    __device__ Scaled(float m_, float unit_) : half(m_ > 1e31f && unit_ < 1e38f ? 0.5f : 1.0f), m(m_ * half), unit(half == 1.0f ? unit_ : unit_ + unit_) {}
+    __device__ float difference(float s) const { return fmaf(s, half, -m); }
+    __device__ float operator()(float s) const { return difference(s) * unit; }
+};
+
 // What a row comes to.
 struct RowSums {
     float m, log_s, h;
@@ -56,7 +65,7 @@ struct RowSums {
         log_s = bad ? __builtin_nanf("") : logf(s);
         h = fmaf(-LN2, a / s, log_s);                     // NaN with log_s
     }
-    __device__ float log_p(float v, float inv_temp) const { return (v - m) * inv_temp - log_s; }
+    __device__ float log_p(float v, float inv_temp) const { return Scaled(m, inv_temp)(v) - log_s; }
 };
 
 // alternative i of the row; key 0: there is none
@@ -131,7 +140,7 @@ template <int DT> __global__ __launch_bounds__(STRETCH_WG, 8) void k_logprobs(Lo
         const float off = -fmaf(from, a.unit, -c), scale = __builtin_amdgcn_exp2f(off);
         elog = scale * fmaf(sum, off, elog);
         sum *= scale;
-    } else {
+    } else {   // (a difference of -Inf: next to c it is thousands below)
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -384,9 +393,10 @@ template <int DT, int R> __global__ __launch_bounds__(ROWS_T) void k_logprobs_ro
     }
     if (wave == 0) {   // the stretches' sums: each lane's, one after the other, then the lanes'
         float sum = 0.f, elog = 0.f;
+        const Scaled scaled(m, a.unit);
         for (int p = lane; p < a.stretches; p += 64) {
             const float from = stretch[3 * p], part = stretch[3 * p + 1];
-            const float x = from == -INFINITY ? -1024.f : fmaxf((from - m) * a.unit, -1024.f), w = __builtin_amdgcn_exp2f(x);
+            const float x = from == -INFINITY ? -1024.f : fmaxf(scaled(from), -1024.f), w = __builtin_amdgcn_exp2f(x);
             sum = fmaf(part, w, sum);
             elog = fmaf(w, fmaf(part, x, stretch[3 * p + 2]), elog);
         }
@@ -518,7 +528,7 @@ template <int DT, int T, bool TOP> __global__ __launch_bounds__(T, 8) void k_log
 #pragma unroll
         for (int n = 0; n < N; ++n) bound.count(bins, bound.bin(g[n]));
     }
-    const float from = m == -INFINITY ? 0.f : m;
+    const Scaled scaled(m == -INFINITY ? 0.f : m, a.unit);
     float sum = 0.f, elog = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -526,7 +536,7 @@ template <int DT, int T, bool TOP> __global__ __launch_bounds__(T, 8) void k_log
         chunk_floats<DT>(f, v[n]);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = (f[e] - from) * a.unit, p = __builtin_amdgcn_exp2f(x);
+            const float x = scaled(f[e]), p = __builtin_amdgcn_exp2f(x);
             sum += p;
             elog = fmaf(p, fmaxf(x, -1024.f), elog);
         }
@@ -665,9 +675,11 @@ template <int DT> __global__ __launch_bounds__(GRAD_T, 8) void k_logprobs_backwa
         return;
     }
     const float inv_s = expf(-log_s), base = log_s - entropy, ca = -total * a.inv_temp, ch = -h * a.inv_temp;
+    const Scaled scaled(m, a.unit);
+    const float unit = scaled.half == 1.0f ? a.inv_temp : a.inv_temp + a.inv_temp;
     const auto dense = [&](float x) {
-        const float d = x - m, p = power(d, a.unit) * inv_s;
-        return p * fmaf(ch, fmaxf(fmaf(d, a.inv_temp, -base), -1024.f), ca);   // log p + H; p is 0 below that
+        const float d = scaled.difference(x), p = power(d, scaled.unit) * inv_s;
+        return p * fmaf(ch, fmaxf(fmaf(d, unit, -base), -1024.f), ca);   // log p + H; p is 0 below that
     };
 #pragma unroll
     for (int n = 0; n < GRAD_N; ++n) {
