@@ -407,7 +407,8 @@ mlmc_status mlmc_quantize(const void *x, int64_t ldx, int64_t rows, int64_t d, i
 /*
  * Linear layer of matrices in 8 bits, a teacher's forward pass: v = (x_scale_n w_scale_m) (x_n . weight_m) + bias, y = act(v) + residual.
  *   x: dev [rows][ldx] bytes, x_scale: dev [rows] fp32;  weight: dev [outputs][ldw] bytes, w_scale: dev [outputs] fp32: as mlmc_quantize and mlmc_rms_norm write them
- *   (any other scales, too);  bias: dev [outputs] fp32 or NULL;  residual: dev [rows][ldr] bf16 or NULL;  y: dev [rows][ldy] bf16 (out; may be residual).
+ *   (any other scales, too; their product is one of fp32: where that is infinite v is infinite or NaN, and what it loses below 2^-126 v loses);
+ *   bias: dev [outputs] fp32 or NULL;  residual: dev [rows][ldr] bf16 or NULL;  y: dev [rows][ldy] bf16 (out; may be residual).
  *   0 <= rows, 1 <= outputs, inputs, each at most 2^21.
  * The matrix units add products in groups and cut what lies more than 12 binary places below the greatest of a group, before the fp32 sum (about 1.5e-5 of a
  * result of normal entries); results have 16 bits for that reason.  Rows whose starts and distances are multiples of 16 bytes are the fastest.

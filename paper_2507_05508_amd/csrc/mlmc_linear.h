@@ -372,7 +372,8 @@ __global__ __launch_bounds__(WM * WN * 64, DT == MLMC_F32 && FM * FN == 1 ? 4 : 
     FA.init(wm * FM);
     FB.init(wn * FN);
     constexpr int Q = PIECES<DT>;
-    // Fragments of two pieces.  Those of 8 bits have twice the registers: a fragment of A is read over as soon as its instructions have gone out (two of each: 424 registers spilled).
+    // Fragments of two pieces.  Those of 8 bits have twice the registers: a fragment of A is read over as soon as its instructions have gone out.  (Of two the tile
+    // of 128 would need 16 registers more; it has 254 of the 256 with which two waves fit on a SIMD.)
     constexpr int PAIR = DT == DT_E4M3 ? 1 : 2;
     fragment_t<DT> fa[PAIR][FM], fb[2][FN];
     const auto read_a = [&](const chunk_t* sa, int m, int q) { fa[q & (PAIR - 1)][m] = FA.get(sa, m, q); };
@@ -729,6 +730,8 @@ static LinearPlan linear_plan(int64_t I, int64_t J, int64_t C, int dtype, bool f
 // take, and the rule goes to tiles (weights in turn, more than the caches hold; 1 row of 4096 inputs: 11008 outputs 18.8 and 21.6, 14336 23.9 and 25.6, 32000 45.7 and 64.0,
 // 131072 169.6 and 176.4; 16 rows: 26.7 and 22.0, where it stays with the few, 32000 65.4 and 65.7, 131072 251 and 182; 4 x 50021 x 512 16.0 and 12.3, where it stays;
 // fp32 1 x 32000 x 1024 29.0 and 36.9): at one row it gives away up to two fifths, at 16 it is right for the longest.
+// Of 8 bits, weights in turn, few rows / tiles: 1 row, 256 outputs of 8192 inputs 7.8 / 14.7, 4096 x 4096 7.8 / 12.8, 8192 x 8192 14.5 / 19.5, 11008 x 4096 13.4 / 14.9, where it takes the few; 32000 x 4096 26.2 / 28.1
+// and 131072 x 4096 92 / 130, where it goes to tiles; 50021 x 512 12.6 / 8.2, where it stays.  16 rows: 4096 x 4096 7.8 / 13.0, 8192 x 8192 20.1 / 19.8, 32000 x 4096 35.3 / 34.7, 131072 x 4096 128 / 133.
 static bool few_rows(int64_t I, int64_t J, int64_t C, int dtype) {
     if (I > FEW_ROWS) return false;
     const float row = (float)C * (float)entry_bytes(dtype), alone = 16.f * row / 3.0e4f, all = (float)J * row / 5.0e6f;
