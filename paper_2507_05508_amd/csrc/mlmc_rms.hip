@@ -355,7 +355,7 @@ template <int DT> __global__ __launch_bounds__(RMS_WG) void k_rms_columns(RmsArg
 
 // Half as many workgroups as the chip holds, each with more rounds for its copy of the weight and the loads ahead; without a weight, and where a thread has one load a round, all of them (us, as many
 // as it holds / half: 8 bits of bf16 8192 x 8192 38 / 48, 20122 x 1880 25 / 28, 4096 x 4096 10.4 / 11.3, of 8000 x 16000 71 / 69.5, of fp32 4096 x 8192 29.7 / 28.9;
-// the norm of bf16 8192 x 8192 46 / 43, 4096 x 4096 15.3 / 13.8, with residual and 8 bits 92 / 88).
+// the norm of bf16 8192 x 8192 50.4 / 46.5, 4096 x 4096 17.3 / 14.4, of 8192 x 8192 with residual and 8 bits 98 / 93).
 template <int DT, int T, int P, bool NORM> static mlmc_status rms_forward_rows(const RmsArgs& a, hipStream_t st) {
     constexpr int WG = T < 256 ? 256 : T, R = WG / T;
     const int64_t all = (a.rows + R - 1) / R, most = (!NORM && P / ENTRIES<DT> == 1 ? 512 : 256) * (1024 / WG);
